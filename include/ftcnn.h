@@ -404,6 +404,121 @@ int ftcnn_relu_pool_encode(int32_t dtype, int32_t n, int32_t c, int32_t h, int32
 int ftcnn_inject(const ftcnn_conv_desc *desc, void *O, const ftcnn_fault *faults, int32_t nf,
                  hipStream_t stream);
 
+/* ---- serving an attention layer -------------------------------------------
+ * The operators between the projections of an attention layer (layers of 1 x 1 maps with the
+ * tokens as the batch), for the new tokens of a batch of sequences whose keys and values live in
+ * a cache of fixed-size pages.  They are not checksum-protected.
+ *
+ * Strides are in elements; the innermost dimension (the `dim` values of a head) is always
+ * contiguous.  dtype (FTCNN_F32 or FTCNN_BF16) is that of every tensor of the call but the
+ * table, the weights (fp32, or the dtype) and the index arrays.  All arithmetic is fp32 or
+ * wider, and results are rounded once (nearest even), except the softmax weights of bf16
+ * attention (see there).  Index arrays are device arrays; what they say is not known to the host:
+ * the kernels bring every index into range, as each call describes, and never leave the
+ * tensors described. */
+
+/* Which values of a head a rotation pairs: (i, i + rot/2), or (2i, 2i + 1), i < rot/2. */
+enum { FTCNN_ROPE_HALF = 0, FTCNN_ROPE_INTERLEAVED = 1 };
+
+/* How angles p * f_j, f_j = base^(-2j/rot), are scaled for longer contexts: not at all; every f_j
+ * divided by factor; base multiplied by factor^(rot/(rot-2)), so that the slowest pair is slowed
+ * by factor and the fastest kept; or by parts: with t = original * f_j / (2 pi) turns within the
+ * `original` positions and keep = clamp((t - low) / (high - low), 0, 1), f_j is multiplied by
+ * keep + (1 - keep) / factor. */
+enum { FTCNN_ROPE_PLAIN = 0, FTCNN_ROPE_LINEAR = 1, FTCNN_ROPE_BASE = 2, FTCNN_ROPE_PARTS = 3 };
+typedef struct {
+    int32_t max_pos, rot;    /* positions, rotated values of a head (even, at most 256) */
+    int32_t scaling;         /* FTCNN_ROPE_PLAIN ..                                     */
+    int32_t original;        /* FTCNN_ROPE_PARTS                                        */
+    double base, factor;     /* factor is not read by FTCNN_ROPE_PLAIN                  */
+    double low, high;        /* FTCNN_ROPE_PARTS                                        */
+    double amplitude;        /* cos and sin are multiplied by it                        */
+} ftcnn_rope_scaling;
+
+/* table[p][j] = (cos, sin) of position p < max_pos and pair j < rot/2, fp32
+ * [max_pos][rot/2][2], evaluated in float64.  Made once, before the application. */
+int ftcnn_rope_table(const ftcnn_rope_scaling *scaling, float *table, hipStream_t stream);
+
+typedef struct {
+    int32_t dtype, tokens;
+    int32_t heads, kv_heads;         /* either may be 0: that tensor is not read          */
+    int32_t dim;                     /* even, at most 256                                 */
+    int32_t rot, layout, max_pos;    /* of the table                                      */
+    int32_t weight_dtype;            /* FTCNN_F32 or dtype                                */
+    float eps;
+    int64_t q_stride[2], k_stride[2], q_out_stride[2], k_out_stride[2];   /* token, head  */
+} ftcnn_rope_desc;
+
+/* Per head of every token: x * rsqrt(mean(x^2) + eps) * weight (no norm where the weight is
+ * NULL), then the rotation of its first rot values by the token's position: a pair (a, b) becomes
+ * (a cos - b sin, b cos + a sin).  positions [tokens] and table go together; both NULL: no
+ * rotation.  The rotated values of a token whose position is not in [0, max_pos) are NaN.
+ * q_out may be q and k_out k (with the same strides); outputs that overlap inputs otherwise are
+ * undefined.  One launch. */
+int ftcnn_qk_norm_rope(const ftcnn_rope_desc *desc, const void *q, const void *k, const int32_t *positions,
+                       const float *table, const void *q_weight, const void *k_weight, void *q_out, void *k_out,
+                       hipStream_t stream);
+
+typedef struct {
+    int32_t dtype, tokens, kv_heads;
+    int32_t dim;                     /* even, at most 256                                 */
+    int32_t rot, layout, max_pos;
+    int32_t weight_dtype;
+    int32_t pages, page;             /* pages of the cache, rows of a page                */
+    float eps;
+    int32_t reserved;
+    int64_t k_stride[2], v_stride[2];               /* token, head                        */
+    int64_t k_cache_stride[3], v_cache_stride[3];   /* page, row, head                    */
+} ftcnn_append_desc;
+
+/* Keys, normed and rotated as ftcnn_qk_norm_rope does it, and values as they are, into the
+ * cache: token t into row slots[t] % page of page slots[t] / page.  A token whose slot is not in
+ * [0, pages * page) (padding: -1) is written nowhere.  Two tokens of one slot leave either's
+ * values.  One launch. */
+int ftcnn_kv_append(const ftcnn_append_desc *desc, const void *k, const void *v, const int32_t *positions,
+                    const float *table, const void *k_weight, const int64_t *slots, void *k_cache, void *v_cache,
+                    hipStream_t stream);
+
+typedef struct {
+    int32_t dtype, batch, tokens;
+    int32_t heads, kv_heads;         /* query head h reads key head h / (heads / kv_heads) */
+    int32_t dim;                     /* a multiple of 8, at most 256                      */
+    int32_t pages, page;             /* pages of the cache, rows of a page (any number)   */
+    int32_t list_len;                /* entries of a sequence's page list                 */
+    int32_t causal, window;          /* window > 0 (causal only): the last window positions */
+    int32_t max_q, max_kv;           /* the longest sequence's new and cached tokens; 0: not
+                                        known.  They size the launch: too small or too large
+                                        costs time, never the result                      */
+    float scale;                     /* positive                                          */
+    int64_t q_stride[2], out_stride[2];             /* token, head                        */
+    int64_t k_cache_stride[3], v_cache_stride[3];   /* page, row, head                    */
+    int64_t list_stride;
+} ftcnn_attention_desc;
+
+/* Attention of every sequence's new tokens over its cached ones.  The new tokens of sequence b
+ * are rows q_starts[b] .. q_starts[b + 1] - 1 of q and out [tokens][heads][dim] (q_starts
+ * [batch + 1], not falling; NULL: row b alone); their keys and values are cached already, as the
+ * last of its kv_lens[b] rows, so that the i-th of n sits at position kv_lens[b] - n + i and sees
+ * positions up to its own (causal), of those the last `window`, or all (not causal).  Position j
+ * lies in row j % page of page page_list[b][j / page].
+ *   out = sum_j softmax_j(scale q . k_j) v_j,   lse = log sum_j exp(scale q . k_j)
+ * with lse (fp32 [tokens][heads], NULL: not wanted) the natural logarithm.  A row that sees
+ * nothing (an empty cache, or fewer cached tokens than new ones) is 0, its lse -infinity.
+ * Scores, maxima, sums and outputs are held in fp32; bf16 calls round the softmax weights,
+ * relative to a maximum, to bf16 for the product with the values.
+ * kv_lens are taken within [0, list_len * page], q_starts within [0, tokens], and a page number
+ * outside [0, pages) as the nearest one inside.  Rows of q, out and the cache start on 16 bytes.
+ * out may be q.  The result does not depend on timing: calls on the same arguments give the same
+ * bits.  One launch, or two where the cached tokens are split over workgroups: then the
+ * workspace holds the parts. */
+int ftcnn_paged_attention(const ftcnn_attention_desc *desc, const void *q, const void *k_cache, const void *v_cache,
+                          const int32_t *page_list, const int32_t *kv_lens, const int32_t *q_starts, void *out,
+                          float *lse, void *workspace, hipStream_t stream);
+
+/* Bytes of 256-byte-aligned workspace that ftcnn_paged_attention takes for this descriptor: 0
+ * where it needs none (NULL will do), and on a bad descriptor. */
+size_t ftcnn_paged_attention_workspace_bytes(const ftcnn_attention_desc *desc);
+
 #ifdef __cplusplus
 }
 #endif

@@ -53,12 +53,39 @@ class Fault(C.Structure):
                 ("kind", C.c_int32), ("bit", C.c_int32), ("value", C.c_double)]
 
 
+class RopeScaling(C.Structure):
+    _fields_ = [("max_pos", C.c_int32), ("rot", C.c_int32), ("scaling", C.c_int32), ("original", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("amplitude", C.c_double)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "heads", "kv_heads", "dim", "rot", "layout", "max_pos",
+                                         "weight_dtype")] + [("eps", C.c_float)] + [
+        (n, C.c_int64 * 2) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")]
+
+
+class AppendDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "kv_heads", "dim", "rot", "layout", "max_pos",
+                                         "weight_dtype", "pages", "page")] + [
+        ("eps", C.c_float), ("reserved", C.c_int32), ("k_stride", C.c_int64 * 2), ("v_stride", C.c_int64 * 2),
+        ("k_cache_stride", C.c_int64 * 3), ("v_cache_stride", C.c_int64 * 3)]
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "batch", "tokens", "heads", "kv_heads", "dim", "pages", "page",
+                                         "list_len", "causal", "window", "max_q", "max_kv")] + [
+        ("scale", C.c_float), ("q_stride", C.c_int64 * 2), ("out_stride", C.c_int64 * 2),
+        ("k_cache_stride", C.c_int64 * 3), ("v_cache_stride", C.c_int64 * 3), ("list_stride", C.c_int64)]
+
+
 EXPORTS = ("ftcnn_out_shape", "ftcnn_workspace_bytes", "ftcnn_report_bytes", "ftcnn_last_error",
            "ftcnn_encode", "ftcnn_conv_fwd", "ftcnn_checksum_conv", "ftcnn_verify", "ftcnn_correct",
            "ftcnn_verify_correct", "ftcnn_conv_fwd_ws", "ftcnn_conv_fwd_sums", "ftcnn_verify_correct_sums", "ftcnn_protected_conv",
            "ftcnn_inject", "ftcnn_set_kernel_events", "ftcnn_conv_fwd_bias", "ftcnn_check_weights",
            "ftcnn_relu_pool", "ftcnn_relu_pool_encode", "ftcnn_conv_fwd_sums_given", "ftcnn_conv_tile",
-           "ftcnn_protected_conv_noalloc", "ftcnn_conv_stream_k")
+           "ftcnn_protected_conv_noalloc", "ftcnn_conv_stream_k", "ftcnn_rope_table", "ftcnn_qk_norm_rope",
+           "ftcnn_kv_append", "ftcnn_paged_attention", "ftcnn_paged_attention_workspace_bytes")
 
 _lib = None
 
@@ -126,5 +153,16 @@ def load(path: str = LIB_PATH):
     L.ftcnn_inject.restype = C.c_int
     L.ftcnn_set_kernel_events.argtypes = [_dp, _dp]
     L.ftcnn_set_kernel_events.restype = C.c_int
+    L.ftcnn_rope_table.argtypes = [P(RopeScaling), _dp, _dp]
+    L.ftcnn_rope_table.restype = C.c_int
+    # descriptors of the serving operators come packed, as bytes in the layout of their structures
+    L.ftcnn_qk_norm_rope.argtypes = [C.c_char_p] + [_dp] * 9
+    L.ftcnn_qk_norm_rope.restype = C.c_int
+    L.ftcnn_kv_append.argtypes = [C.c_char_p] + [_dp] * 9
+    L.ftcnn_kv_append.restype = C.c_int
+    L.ftcnn_paged_attention.argtypes = [C.c_char_p] + [_dp] * 10
+    L.ftcnn_paged_attention.restype = C.c_int
+    L.ftcnn_paged_attention_workspace_bytes.argtypes = [C.c_char_p]
+    L.ftcnn_paged_attention_workspace_bytes.restype = C.c_size_t
     _lib = L
     return L

@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "ftcnn_internal.h"
+#include "paged.h"
 
 namespace ftcnn {
 namespace {
@@ -25,6 +26,18 @@ int fail(int code, const char *fmt, ...) {
 int hip_fail(hipError_t e, const char *where) {
     return fail(FTCNN_E_HIP, "%s: %s", where, hipGetErrorString(e));
 }
+
+}  // namespace
+
+int set_error(int code, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof g_err, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+namespace {
 
 size_t align256(size_t b) { return (b + 255) & ~size_t(255); }
 

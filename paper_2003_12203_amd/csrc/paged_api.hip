@@ -1,0 +1,298 @@
+// The C entry points of the serving operators (include/ftcnn.h): argument checks and the launch plan.
+#include <math.h>
+
+#include <algorithm>
+
+#include "paged.h"
+
+namespace ftcnn {
+namespace {
+
+#define FT_PAGED_HIP(expr, where)                                                        \
+    do {                                                                                 \
+        const hipError_t _e = (expr);                                                    \
+        if (_e != hipSuccess) return set_error(FTCNN_E_HIP, "%s: %s", where, hipGetErrorString(_e)); \
+    } while (0)
+
+constexpr long long kMaxRows = 1LL << 30;   // rows a sequence's page list can name, and rows of queries
+
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+int check_dtype(int32_t dtype, const char *what) {
+    if (dtype != FTCNN_F32 && dtype != FTCNN_BF16) return set_error(FTCNN_E_DTYPE, "%s: dtype %d", what, dtype);
+    return FTCNN_OK;
+}
+
+// What the two rotating operators share: sizes, the rotation, the weights.
+int check_rope(const char *what, int32_t dtype, int32_t tokens, int32_t heads, int32_t dim, int32_t rot,
+               int32_t layout, int32_t max_pos, float eps, const void *positions, const void *table,
+               bool normed, int32_t weight_dtype) {
+    const int rc = check_dtype(dtype, what);
+    if (rc != FTCNN_OK) return rc;
+    if (tokens < 0 || heads < 1 || dim < 2 || dim > 256 || dim % 2)
+        return set_error(FTCNN_E_SHAPE, "%s: tokens %d, heads %d, dim %d (even, at most 256)", what, tokens, heads,
+                         dim);
+    if ((long long)tokens * heads > kMaxRows) return set_error(FTCNN_E_SHAPE, "%s: more than 2^30 rows", what);
+    if (!positions != !table) return set_error(FTCNN_E_ARG, "%s: positions and table go together", what);
+    if (positions) {
+        if (rot < 2 || rot % 2 || rot > dim)
+            return set_error(FTCNN_E_SHAPE, "%s: rot %d (even, 2 to dim = %d)", what, rot, dim);
+        if (max_pos < 1) return set_error(FTCNN_E_SHAPE, "%s: max_pos %d", what, max_pos);
+        if (layout != FTCNN_ROPE_HALF && layout != FTCNN_ROPE_INTERLEAVED)
+            return set_error(FTCNN_E_ARG, "%s: layout %d", what, layout);
+    }
+    if (normed) {
+        if (!(eps >= 0.0f) || !std::isfinite(eps)) return set_error(FTCNN_E_ARG, "%s: eps %g", what, (double)eps);
+        if (weight_dtype != FTCNN_F32 && weight_dtype != dtype)
+            return set_error(FTCNN_E_DTYPE, "%s: weights of dtype %d (fp32, or the tensors')", what, weight_dtype);
+    }
+    return FTCNN_OK;
+}
+
+}  // namespace
+
+AttnPlan attn_plan(const ftcnn_attention_desc &d) {
+    AttnPlan p{};
+    const long long group = d.heads / d.kv_heads, capacity = (long long)d.list_len * d.page;
+    const long long max_q = std::max(1LL, std::min<long long>(d.max_q > 0 ? d.max_q : d.tokens, d.tokens));
+    const long long max_kv = std::max(1LL, std::min(d.max_kv > 0 ? d.max_kv : capacity, capacity));
+    const long long rows = max_q * group;
+    p.dp = d.dim <= 64 ? 64 : (d.dim <= 128 ? 128 : 256);
+    if (d.dtype == FTCNN_F32) {
+        p.wr = rows <= 32 ? 1 : 4;
+        p.wk = p.wr > 1 ? 1 : (p.dp > 128 ? 1 : (p.dp > 64 ? 2 : 4));
+    } else {
+        p.wr = rows <= 32 ? 1 : (rows <= 64 ? 2 : (p.dp > 128 ? 4 : 8));
+        p.wk = p.wr > 2 ? 1 : (p.wr == 2 ? 2 : (p.dp > 128 ? 2 : 4));
+    }
+    const long long tile = 32 * p.wr;
+    p.tiles = (int)((rows + tile - 1) / tile);
+    const long long some = std::min<long long>((long long)d.batch * p.tiles, d.tokens * group / tile + d.batch);
+    const long long groups = std::max(1LL, some * d.kv_heads);
+    const long long range = d.window > 0 ? std::min<long long>(max_kv, (long long)d.window + tile / group + 1) : max_kv;
+    const long long want = (512 + groups - 1) / groups;
+    long long per = (range + want - 1) / want;
+    per = std::max<long long>(per, p.wr > 2 ? 1024 : 512);
+    if (p.wr <= 2) per = std::min<long long>(per, 2048);
+    per = (per + 127) / 128 * 128;
+    p.splits = (int)((range + per - 1) / per);
+    p.per_split = (int)per;
+    if (p.splits > 1) {
+        const size_t n = (size_t)d.tokens * d.heads * p.splits;
+        p.part_o = (n * d.dim * sizeof(float) + 255) & ~size_t(255);
+        p.bytes = p.part_o + ((n * 2 * sizeof(float) + 255) & ~size_t(255));
+    }
+    return p;
+}
+
+namespace {
+
+int check_attention(const ftcnn_attention_desc *d) {
+    const char *what = "paged_attention";
+    if (!d) return set_error(FTCNN_E_ARG, "%s: null descriptor", what);
+    const int rc = check_dtype(d->dtype, what);
+    if (rc != FTCNN_OK) return rc;
+    if (d->batch < 0 || d->tokens < 0 || d->heads < 1 || d->kv_heads < 1 || d->pages < 1 || d->page < 1 ||
+        d->list_len < 0 || d->max_q < 0 || d->max_kv < 0)
+        return set_error(FTCNN_E_SHAPE, "%s: non-positive size", what);
+    if (d->heads % d->kv_heads)
+        return set_error(FTCNN_E_SHAPE, "%s: %d key heads do not divide %d heads", what, d->kv_heads, d->heads);
+    if (d->dim < 8 || d->dim > 256 || d->dim % 8)
+        return set_error(FTCNN_E_UNSUPPORTED, "%s: dim %d (a multiple of 8, at most 256)", what, d->dim);
+    if ((long long)d->tokens * d->heads > kMaxRows || (long long)d->list_len * d->page > kMaxRows)
+        return set_error(FTCNN_E_SHAPE, "%s: more than 2^30 rows", what);
+    if (d->window < 0 || (d->window > 0 && !d->causal))
+        return set_error(FTCNN_E_ARG, "%s: window %d (0, or positive with causal)", what, d->window);
+    if (!(d->scale > 0.0f) || !std::isfinite(d->scale))
+        return set_error(FTCNN_E_ARG, "%s: scale %g (positive)", what, (double)d->scale);
+    return FTCNN_OK;
+}
+
+}  // namespace
+}  // namespace ftcnn
+
+using namespace ftcnn;
+
+extern "C" {
+
+int ftcnn_rope_table(const ftcnn_rope_scaling *sc, float *table, hipStream_t stream) {
+    if (!sc || !table) return set_error(FTCNN_E_ARG, "rope_table: null pointer");
+    if (sc->max_pos < 1 || sc->rot < 2 || sc->rot % 2 || sc->rot > 256)
+        return set_error(FTCNN_E_SHAPE, "rope_table: max_pos %d, rot %d (even, at most 256)", sc->max_pos, sc->rot);
+    if (sc->scaling < FTCNN_ROPE_PLAIN || sc->scaling > FTCNN_ROPE_PARTS)
+        return set_error(FTCNN_E_ARG, "rope_table: scaling %d", sc->scaling);
+    if (!(sc->base > 0.0) || !std::isfinite(sc->base) || !std::isfinite(sc->amplitude))
+        return set_error(FTCNN_E_ARG, "rope_table: base %g, amplitude %g", sc->base, sc->amplitude);
+    if (sc->scaling != FTCNN_ROPE_PLAIN && (!(sc->factor > 0.0) || !std::isfinite(sc->factor)))
+        return set_error(FTCNN_E_ARG, "rope_table: factor %g", sc->factor);
+    if (sc->scaling == FTCNN_ROPE_PARTS && (sc->original < 1 || !(sc->high > sc->low) || !std::isfinite(sc->low) ||
+                                            !std::isfinite(sc->high)))
+        return set_error(FTCNN_E_ARG, "rope_table: original %d, low %g, high %g", sc->original, sc->low, sc->high);
+    FT_PAGED_HIP(launch_rope_table(*sc, table, stream), "rope_table");
+    return FTCNN_OK;
+}
+
+int ftcnn_qk_norm_rope(const ftcnn_rope_desc *d, const void *q, const void *k, const int32_t *positions,
+                       const float *table, const void *q_weight, const void *k_weight, void *q_out, void *k_out,
+                       hipStream_t stream) {
+    const char *what = "qk_norm_rope";
+    if (!d) return set_error(FTCNN_E_ARG, "%s: null descriptor", what);
+    if (d->heads < 0 || d->kv_heads < 0) return set_error(FTCNN_E_SHAPE, "%s: negative heads", what);
+    const int rc = check_rope(what, d->dtype, d->tokens, d->heads + d->kv_heads, d->dim, d->rot, d->layout,
+                              d->max_pos, d->eps, positions, table, q_weight || k_weight, d->weight_dtype);
+    if (rc != FTCNN_OK) return rc;
+    if (d->tokens == 0) return FTCNN_OK;
+    if ((d->heads && (!q || !q_out)) || (d->kv_heads && (!k || !k_out)))
+        return set_error(FTCNN_E_ARG, "%s: null pointer", what);
+    RopeArgs a{};
+    const void *in[2] = {q, k}, *wt[2] = {q_weight, k_weight};
+    void *out[2] = {q_out, k_out};
+    const int32_t heads[2] = {d->heads, d->kv_heads};
+    const int64_t *is[2] = {d->q_stride, d->k_stride}, *os[2] = {d->q_out_stride, d->k_out_stride};
+    const int vec = d->dtype == FTCNN_F32 ? 4 : 8;
+    bool al = d->dim % (2 * vec) == 0 && (!positions || (d->rot % (2 * vec) == 0 && aligned16(table)));
+    for (int s = 0; s < 2; ++s) {
+        a.x[s] = in[s];
+        a.y[s] = out[s];
+        a.weight[s] = wt[s];
+        a.heads[s] = heads[s];
+        for (int i = 0; i < 2; ++i) {
+            a.xs[s][i] = is[s][i];
+            a.ys[s][i] = os[s][i];
+            al = al && (!heads[s] || (is[s][i] % vec == 0 && os[s][i] % vec == 0));
+        }
+        al = al && (!heads[s] || (aligned16(in[s]) && aligned16(out[s])));
+    }
+    a.tokens = d->tokens;
+    a.dim = d->dim;
+    a.rot = positions ? d->rot : 0;
+    a.max_pos = d->max_pos;
+    a.interleaved = d->layout == FTCNN_ROPE_INTERLEAVED;
+    a.weight_f32 = d->weight_dtype == FTCNN_F32;
+    a.eps = d->eps;
+    a.positions = positions;
+    a.table = table;
+    FT_PAGED_HIP(launch_rope(d->dtype, a, al, stream), what);
+    return FTCNN_OK;
+}
+
+int ftcnn_kv_append(const ftcnn_append_desc *d, const void *k, const void *v, const int32_t *positions,
+                    const float *table, const void *k_weight, const int64_t *slots, void *k_cache, void *v_cache,
+                    hipStream_t stream) {
+    const char *what = "kv_append";
+    if (!d) return set_error(FTCNN_E_ARG, "%s: null descriptor", what);
+    const int rc = check_rope(what, d->dtype, d->tokens, d->kv_heads, d->dim, d->rot, d->layout, d->max_pos, d->eps,
+                              positions, table, k_weight != nullptr, d->weight_dtype);
+    if (rc != FTCNN_OK) return rc;
+    if (d->pages < 1 || d->page < 1)
+        return set_error(FTCNN_E_SHAPE, "%s: %d pages of %d rows", what, d->pages, d->page);
+    if (d->tokens == 0) return FTCNN_OK;
+    if (!k || !v || !slots || !k_cache || !v_cache) return set_error(FTCNN_E_ARG, "%s: null pointer", what);
+    RopeArgs a{};
+    const void *in[2] = {k, v};
+    void *out[2] = {k_cache, v_cache};
+    const int64_t *is[2] = {d->k_stride, d->v_stride}, *os[2] = {d->k_cache_stride, d->v_cache_stride};
+    const int vec = d->dtype == FTCNN_F32 ? 4 : 8;
+    bool al = d->dim % (2 * vec) == 0 && (!positions || (d->rot % (2 * vec) == 0 && aligned16(table)));
+    for (int s = 0; s < 2; ++s) {
+        a.x[1 + s] = in[s];
+        a.y[1 + s] = out[s];
+        a.heads[1 + s] = d->kv_heads;
+        for (int i = 0; i < 3; ++i) {
+            if (i < 2) {
+                a.xs[1 + s][i] = is[s][i];
+                al = al && is[s][i] % vec == 0;
+            }
+            a.ys[1 + s][i] = os[s][i];
+            al = al && os[s][i] % vec == 0;
+        }
+        al = al && aligned16(in[s]) && aligned16(out[s]);
+    }
+    a.weight[1] = k_weight;
+    a.tokens = d->tokens;
+    a.dim = d->dim;
+    a.rot = positions ? d->rot : 0;
+    a.max_pos = d->max_pos;
+    a.interleaved = d->layout == FTCNN_ROPE_INTERLEAVED;
+    a.weight_f32 = d->weight_dtype == FTCNN_F32;
+    a.pages = d->pages;
+    a.page = d->page;
+    a.eps = d->eps;
+    a.positions = positions;
+    a.slots = slots;
+    a.table = table;
+    FT_PAGED_HIP(launch_rope(d->dtype, a, al, stream), what);
+    return FTCNN_OK;
+}
+
+size_t ftcnn_paged_attention_workspace_bytes(const ftcnn_attention_desc *desc) {
+    return check_attention(desc) == FTCNN_OK && desc->tokens > 0 ? attn_plan(*desc).bytes : 0;
+}
+
+int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const void *k_cache, const void *v_cache,
+                          const int32_t *page_list, const int32_t *kv_lens, const int32_t *q_starts, void *out,
+                          float *lse, void *workspace, hipStream_t stream) {
+    const char *what = "paged_attention";
+    const int rc = check_attention(d);
+    if (rc != FTCNN_OK) return rc;
+    if (!q_starts && d->tokens != d->batch)
+        return set_error(FTCNN_E_SHAPE, "%s: %d tokens of %d sequences need q_starts", what, d->tokens, d->batch);
+    if (d->tokens == 0 || d->batch == 0) return FTCNN_OK;
+    if (!q || !k_cache || !v_cache || !kv_lens || !out || (!page_list && d->list_len))
+        return set_error(FTCNN_E_ARG, "%s: null pointer", what);
+    const int vec = d->dtype == FTCNN_F32 ? 4 : 8;
+    bool al = aligned16(q) && aligned16(k_cache) && aligned16(v_cache) && aligned16(out);
+    for (int i = 0; i < 3; ++i) {
+        if (i < 2) al = al && d->q_stride[i] % vec == 0 && d->out_stride[i] % vec == 0;
+        al = al && d->k_cache_stride[i] % vec == 0 && d->v_cache_stride[i] % vec == 0;
+    }
+    if (!al)
+        return set_error(FTCNN_E_UNSUPPORTED, "%s: rows of q, out and the cache must start on 16 bytes", what);
+    const AttnPlan pl = attn_plan(*d);
+    if (pl.bytes && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256))
+        return set_error(FTCNN_E_WORKSPACE, "%s: workspace missing or not 256-byte aligned", what);
+    const long long blocks = (long long)pl.tiles * pl.splits * d->kv_heads * d->batch;
+    if (blocks > 0x7fffffffLL) return set_error(FTCNN_E_SHAPE, "%s: %lld workgroups", what, blocks);
+    AttnArgs a{};
+    a.q = q;
+    a.k = k_cache;
+    a.v = v_cache;
+    a.o = out;
+    a.lse = lse;
+    a.part_o = static_cast<float *>(workspace);
+    a.part_ml = workspace ? reinterpret_cast<float *>(static_cast<char *>(workspace) + pl.part_o) : nullptr;
+    a.page_list = page_list;
+    a.kv_lens = kv_lens;
+    a.q_starts = q_starts;
+    for (int i = 0; i < 3; ++i) {
+        if (i < 2) {
+            a.qs[i] = d->q_stride[i];
+            a.os[i] = d->out_stride[i];
+        }
+        a.ks[i] = d->k_cache_stride[i];
+        a.vs[i] = d->v_cache_stride[i];
+    }
+    a.list_stride = d->list_stride;
+    a.batch = d->batch;
+    a.tokens = d->tokens;
+    a.kv_heads = d->kv_heads;
+    a.group = d->heads / d->kv_heads;
+    a.dim = d->dim;
+    a.pages = d->pages;
+    a.page = d->page;
+    a.capacity = d->list_len * d->page;
+    a.causal = d->causal != 0;
+    a.window = d->window;
+    a.tiles = pl.tiles;
+    a.splits = pl.splits;
+    a.per_split = pl.per_split;
+    a.interleave = pl.tiles > 1 && (long long)d->batch * d->kv_heads % 8 == 0;
+    a.div_page = fast_div((uint32_t)d->page);
+    a.div_group = fast_div((uint32_t)a.group);
+    a.scale_log2 = d->scale * 1.44269504088896340736f;
+    FT_PAGED_HIP(d->dtype == FTCNN_F32 ? launch_attn_f32(pl, a, stream) : launch_attn_bf16(pl, a, stream), what);
+    if (pl.splits > 1) FT_PAGED_HIP(launch_attn_join(d->dtype, pl, a, stream), "paged_attention: join");
+    return FTCNN_OK;
+}
+
+}  // extern "C"

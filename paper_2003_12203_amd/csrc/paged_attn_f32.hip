@@ -1,0 +1,19 @@
+// fp32 instances of the attention kernel.
+#include "paged_attn.h"
+
+namespace ftcnn {
+namespace {
+template <int DP> hipError_t pick(const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
+    constexpr int WK = DP == 64 ? 4 : (DP == 128 ? 2 : 1);
+    if (pl.wr == 1) return attn_go<float, DP, 1, WK, 1>(a, st);
+    return attn_go<float, DP, 4, 1, 1>(a, st);
+}
+}  // namespace
+
+hipError_t launch_attn_f32(const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
+    if (pl.dp == 64) return pick<64>(pl, a, st);
+    if (pl.dp == 128) return pick<128>(pl, a, st);
+    return pick<256>(pl, a, st);
+}
+
+}  // namespace ftcnn

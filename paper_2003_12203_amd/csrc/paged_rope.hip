@@ -1,0 +1,246 @@
+// Norms of queries and keys for each head with the rotation by position, and keys and values
+// written to a paged cache with the same on the way.
+//
+// A row is one head of one token: y = x * rsqrt(mean(x^2) + eps) * weight (with a weight), then
+// every pair (a, b) of its first `rot` values becomes (a cos - b sin, b cos + a sin); the rest of
+// the row is kept.  In fp32, rounded once.  Pairs are (i, i + rot/2) ("half") or (2i, 2i + 1)
+// ("interleaved"); (cos, sin) of a pair at a position come from a table made once in float64.
+//
+// Memory-bound: a row is read and written once, and the table's row once for several heads.  A row is
+// cut into units of two vectors of V values (16 bytes each where alignment allows): a rotated unit
+// holds V whole pairs, so a rotation needs no other lane.  A group of lanes holds a row, a unit or
+// more a lane, and walks some heads of a token, four rows in flight.
+#include <algorithm>
+
+#include "paged.h"
+
+namespace ftcnn {
+namespace {
+
+template <typename T, int V> struct Vec;
+template <> struct Vec<float, 4> { typedef uint4 type; };
+template <> struct Vec<uint16_t, 8> { typedef uint4 type; };
+template <> struct Vec<float, 1> { typedef float type; };
+template <> struct Vec<uint16_t, 1> { typedef uint16_t type; };
+
+template <typename T, int V> union Pack {
+    typename Vec<T, V>::type q;
+    T e[V];
+};
+
+__device__ inline float as_f32(float v) { return v; }
+__device__ inline float as_f32(uint16_t v) { return bf16_bits_to_f32(v); }
+__device__ inline void put(float &d, float v) { d = v; }
+__device__ inline void put(uint16_t &d, float v) { d = f32_to_bf16_rne(v); }
+
+constexpr int kRowsInFlight = 4;
+
+// LPR lanes hold a row, UPL units a lane (unit lane + u * LPR).
+template <typename T, int V, int LPR, int UPL>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
+    constexpr int B = UPL == 1 ? kRowsInFlight : 1;
+    const int lane = threadIdx.x % LPR;
+    const unsigned id = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
+    const unsigned token = div_by(id, a.div_chunks);
+    int chunk = (int)(id - token * (unsigned)a.all_chunks);
+    if (token >= (unsigned)a.tokens) return;
+    int sec = 0;
+    while (chunk >= a.chunks[sec]) chunk -= a.chunks[sec++];   // all_chunks is their sum
+    const T *x = static_cast<const T *>(a.x[sec]) + (long long)token * a.xs[sec][0];
+    T *y = static_cast<T *>(a.y[sec]);
+    long long yh = a.ys[sec][1];
+    if (a.slots) {
+        const int64_t slot = a.slots[token];
+        if (slot < 0 || slot >= (int64_t)a.pages * a.page) return;   // written nowhere
+        const int64_t pg = slot / a.page;
+        y += pg * a.ys[sec][0] + (slot - pg * a.page) * a.ys[sec][1];
+        yh = a.ys[sec][2];
+    } else {
+        y += (long long)token * a.ys[sec][0];
+    }
+    const bool normed = sec < 2 && a.weight[sec];
+    const bool rotated = sec < 2 && a.positions;
+    const int units = a.dim / (2 * V), turned = rotated ? a.rot / (2 * V) : 0;
+    int offa[UPL], offb[UPL];
+    bool mine[UPL];
+    float cs[UPL][2 * V], w[UPL][2 * V];
+#pragma unroll
+    for (int u = 0; u < UPL; ++u) {
+        const int k = lane + u * LPR;
+        mine[u] = k < units;
+        const bool half = k < turned && !a.interleaved;
+        offa[u] = half ? k * V : 2 * k * V;
+        offb[u] = half ? a.rot / 2 + k * V : (2 * k + 1) * V;
+        if (k < turned) {
+            const int pos = a.positions[token];
+            if (pos >= 0 && pos < a.max_pos) {
+                const float *t = a.table + (long long)pos * a.rot + 2 * k * V;
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) cs[u][i] = t[i];
+            } else {   // no such position
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) cs[u][i] = __builtin_nanf("");
+            }
+        }
+        if (normed && mine[u]) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (a.weight_f32) {
+                    const float *g = static_cast<const float *>(a.weight[sec]);
+                    w[u][i] = g[offa[u] + i];
+                    w[u][V + i] = g[offb[u] + i];
+                } else {
+                    const T *g = static_cast<const T *>(a.weight[sec]);
+                    w[u][i] = as_f32(g[offa[u] + i]);
+                    w[u][V + i] = as_f32(g[offb[u] + i]);
+                }
+            }
+        }
+    }
+    const int first = chunk * a.per_chunk, last = min(first + a.per_chunk, a.heads[sec]);
+    for (int h0 = first; h0 < last; h0 += B) {
+        Pack<T, V> pa[B][UPL], pb[B][UPL];
+#pragma unroll
+        for (int r = 0; r < B; ++r) {
+            const T *row = x + (long long)min(h0 + r, last - 1) * a.xs[sec][1];
+#pragma unroll
+            for (int u = 0; u < UPL; ++u)
+                if (mine[u]) {
+                    pa[r][u].q = *reinterpret_cast<const typename Vec<T, V>::type *>(row + offa[u]);
+                    pb[r][u].q = *reinterpret_cast<const typename Vec<T, V>::type *>(row + offb[u]);
+                }
+        }
+#pragma unroll
+        for (int r = 0; r < B; ++r) {
+            if (h0 + r >= last) break;
+            T *row = y + (long long)(h0 + r) * yh;
+            float scale = 1.0f;
+            if (normed) {
+                float ss = 0.0f;
+#pragma unroll
+                for (int u = 0; u < UPL; ++u)
+                    if (mine[u])
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            const float va = as_f32(pa[r][u].e[i]), vb = as_f32(pb[r][u].e[i]);
+                            ss = fmaf(va, va, ss);
+                            ss = fmaf(vb, vb, ss);
+                        }
+#pragma unroll
+                for (int m = LPR / 2; m > 0; m /= 2) ss += __shfl_xor(ss, m, LPR);
+                scale = rsqrtf(ss / (float)a.dim + a.eps);
+            }
+#pragma unroll
+            for (int u = 0; u < UPL; ++u) {
+                if (!mine[u]) continue;
+                const bool turn = lane + u * LPR < turned;
+                if (normed || turn) {
+                    float f[2 * V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        f[i] = as_f32(pa[r][u].e[i]);
+                        f[V + i] = as_f32(pb[r][u].e[i]);
+                    }
+                    if (normed)
+#pragma unroll
+                        for (int i = 0; i < 2 * V; ++i) f[i] = f[i] * scale * w[u][i];
+                    if (turn) {
+#pragma unroll
+                        for (int p = 0; p < V; ++p) {
+                            const float c = cs[u][2 * p], s = cs[u][2 * p + 1];
+                            // a vector's neighbours, or the two vectors' values of the same index
+                            const float n0 = f[2 * p], n1 = f[2 * p + 1], h0v = f[p], h1v = f[V + p];
+                            const float va = a.interleaved ? n0 : h0v, vb = a.interleaved ? n1 : h1v;
+                            const float ra = va * c - vb * s, rb = vb * c + va * s;
+                            const int ia = 2 * p, ib = 2 * p + 1;
+                            if (a.interleaved) {
+                                put(ia < V ? pa[r][u].e[ia] : pb[r][u].e[ia - V], ra);
+                                put(ib < V ? pa[r][u].e[ib] : pb[r][u].e[ib - V], rb);
+                            } else {
+                                put(pa[r][u].e[p], ra);
+                                put(pb[r][u].e[p], rb);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            put(pa[r][u].e[i], f[i]);
+                            put(pb[r][u].e[i], f[V + i]);
+                        }
+                    }
+                }
+                *reinterpret_cast<typename Vec<T, V>::type *>(row + offa[u]) = pa[r][u].q;
+                *reinterpret_cast<typename Vec<T, V>::type *>(row + offb[u]) = pb[r][u].q;
+            }
+        }
+    }
+}
+
+template <typename T, int V, int LPR, int UPL>
+hipError_t go(RopeArgs a, hipStream_t st) {
+    const long long rows = a.heads[0] + a.heads[1] + a.heads[2];
+    // heads a group: enough to read a table row for several, few enough that the device is full
+    // (a wave for each of its 1024 SIMDs, eight over)
+    const long long groups = 8192LL * (64 / LPR);
+    a.per_chunk = (int)std::min<long long>(8, std::max<long long>(1, a.tokens * rows / groups));
+    a.all_chunks = 0;
+    for (int s = 0; s < 3; ++s) a.all_chunks += a.chunks[s] = (a.heads[s] + a.per_chunk - 1) / a.per_chunk;
+    a.div_chunks = fast_div((uint32_t)a.all_chunks);
+    const long long ids = (long long)a.tokens * a.all_chunks;
+    const long long blocks = (ids + kThreads / LPR - 1) / (kThreads / LPR);
+    if (ids >= (1LL << 31)) return hipErrorInvalidValue;
+    rope_kernel<T, V, LPR, UPL><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int V> hipError_t pick(const RopeArgs &a, hipStream_t st) {
+    const int units = a.dim / (2 * V);
+    if constexpr (V > 1) {
+        if (units <= 4) return go<T, V, 4, 1>(a, st);
+        if (units <= 8) return go<T, V, 8, 1>(a, st);
+        if (units <= 16) return go<T, V, 16, 1>(a, st);
+        return go<T, V, 32, 1>(a, st);
+    } else {
+        if (units <= 32) return go<T, V, 32, 1>(a, st);
+        if (units <= 64) return go<T, V, 64, 1>(a, st);
+        return go<T, V, 64, 2>(a, st);
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void rope_table_kernel(ftcnn_rope_scaling sc, float2 *table) {
+    const int half = sc.rot / 2;
+    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= (long long)sc.max_pos * half) return;
+    const int pos = (int)(i / half), j = (int)(i % half);
+    constexpr double two_pi = 6.283185307179586476925;
+    const double base = sc.scaling == FTCNN_ROPE_BASE && sc.rot > 2
+                            ? sc.base * pow(sc.factor, sc.rot / (sc.rot - 2.0)) : sc.base;
+    double f = pow(base, -2.0 * j / sc.rot);
+    if (sc.scaling == FTCNN_ROPE_LINEAR) {
+        f /= sc.factor;
+    } else if (sc.scaling == FTCNN_ROPE_PARTS) {
+        const double turns = sc.original * f / two_pi;
+        double keep = (turns - sc.low) / (sc.high - sc.low);
+        keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+        f *= keep + (1.0 - keep) / sc.factor;
+    }
+    double s, c;
+    sincos(pos * f, &s, &c);
+    table[i] = make_float2((float)(c * sc.amplitude), (float)(s * sc.amplitude));
+}
+
+}  // namespace
+
+hipError_t launch_rope(int dtype, RopeArgs a, bool aligned, hipStream_t st) {
+    if (dtype == FTCNN_F32) return aligned ? pick<float, 4>(a, st) : pick<float, 1>(a, st);
+    return aligned ? pick<uint16_t, 8>(a, st) : pick<uint16_t, 1>(a, st);
+}
+
+hipError_t launch_rope_table(const ftcnn_rope_scaling &sc, float *table, hipStream_t st) {
+    const long long n = (long long)sc.max_pos * (sc.rot / 2);
+    rope_table_kernel<<<(unsigned)((n + kThreads - 1) / kThreads), kThreads, 0, st>>>(
+        sc, reinterpret_cast<float2 *>(table));
+    return hipGetLastError();
+}
+
+}  // namespace ftcnn

@@ -1,0 +1,363 @@
+"""The operators of a serving attention layer on the GPU against their definitions in float64
+(oracle.serving), each element within the bound that fp32 arithmetic and the outputs' rounding keep to."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2003_12203_amd as ft
+from oracle import serving as sv
+from paper_2003_12203_amd import paged
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def normal(rng, shape, dtype, scale=1.0):
+    return torch.from_numpy((rng.standard_normal(shape) * scale).astype(np.float32)).to(DT[dtype]).cuda()
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def near(got, want, bound, what=""):
+    got = f64(got) if isinstance(got, torch.Tensor) else got
+    assert got.shape == want.shape, what
+    assert np.array_equal(np.isnan(got), np.isnan(want)), f"{what}: NaN in other places"
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf]) and not np.isinf(got[~inf]).any(), f"{what}: infinities"
+    ok = np.isfinite(want)
+    over = np.abs(got[ok] - want[ok]) - bound[ok]
+    if over.size:
+        assert over.max() <= 0, f"{what}: {int((over > 0).sum())} of {over.size} beyond their bound, by {over.max()}"
+
+
+# ---- the table -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kw", [
+    dict(max_pos=1, rot=2), dict(max_pos=700, rot=64), dict(max_pos=300, rot=128, base=500000.0),
+    dict(max_pos=300, rot=96, scaling="linear", factor=8.0), dict(max_pos=300, rot=64, scaling="base", factor=4.0),
+    dict(max_pos=2, rot=2, scaling="base", factor=4.0),
+    dict(max_pos=300, rot=128, scaling="parts", factor=4.0, original=4096, amplitude=1.1386),
+    dict(max_pos=131072, rot=4, scaling="parts", factor=32.0, original=4096, low=1.0, high=16.0)])
+def test_rope_table(kw):
+    got, want = f64(paged.rope_table(**kw)), sv.rope_table(**kw)
+    # float64 angles up to 2^17 are within 2^-35 of each other; one rounding to fp32
+    near(got, want, np.abs(want) * sv.U32 + 2.0 ** -33 * kw.get("amplitude", 1.0))
+
+
+# ---- norms and rotation ------------------------------------------------------------------------------
+
+ROPE = [  # tokens, heads, kv_heads, dim, rot, layout, norm
+    (1, 1, 1, 2, 2, "half", True), (1, 4, 2, 128, 128, "half", True), (3, 5, 1, 64, 64, "interleaved", True),
+    (130, 8, 2, 128, 64, "half", False), (17, 3, 3, 80, 32, "interleaved", True), (5, 2, 1, 96, 90, "half", True),
+    (5, 2, 1, 96, 90, "interleaved", True), (33, 2, 2, 256, 256, "half", True), (9, 1, 1, 254, 10, "half", True),
+    (65, 12, 4, 72, 72, "interleaved", False), (700, 8, 8, 48, 16, "half", True), (2, 32, 0, 128, 128, "half", True),
+    (2, 0, 8, 128, 128, "half", True), (7, 2, 2, 6, 4, "interleaved", True), (4, 2, 2, 128, 0, "half", True),
+    (4, 2, 2, 128, 0, "half", False)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,heads,kv,dim,rot,layout,norm", ROPE)
+def test_qk_norm_rope(dtype, tokens, heads, kv, dim, rot, layout, norm):
+    rng = np.random.default_rng([tokens, heads, dim, rot])
+    packed = normal(rng, (tokens, (heads + 2 * kv) * dim), dtype)
+    q = packed[:, :heads * dim].view(tokens, heads, dim) if heads else None
+    k = packed[:, heads * dim:(heads + kv) * dim].view(tokens, kv, dim) if kv else None
+    table = positions = None
+    if rot:
+        table = paged.rope_table(500, rot)
+        positions = torch.from_numpy(rng.integers(0, 500, tokens).astype(np.int32)).cuda()
+    qw = normal(rng, (dim,), dtype) if norm else None
+    kw = normal(rng, (dim,), dtype) if norm else None
+    got = paged.qk_norm_rope(q, k, positions, table, qw if heads else None, kw if kv else None, layout=layout)
+    args = (positions.cpu().numpy(), f64(table)) if rot else (None, None)
+    for x, w, y in ((q, qw, got[0]), (k, kw, got[1])):
+        if x is None:
+            assert y is None
+            continue
+        want, bound = sv.norm_rope(f64(x), *args, None if w is None else f64(w), 1e-6, layout, dtype)
+        near(y, want, bound)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_qk_norm_rope_in_place_and_strided(dtype):
+    rng = np.random.default_rng(5)
+    x = normal(rng, (20, 6, 130), dtype)          # rows that start off 16 bytes
+    q, k = x[:, :4, 1:129], x[:, 4:, 1:129]
+    table, pos = paged.rope_table(64, 128), torch.arange(20, dtype=torch.int32, device="cuda")
+    w = normal(rng, (128,), "f32")                # fp32 weights beside either dtype
+    want = [sv.norm_rope(f64(t), range(20), f64(table), f64(w), 1e-5, "half", dtype) for t in (q, k)]
+    edges = x[:, :, 0].clone(), x[:, :, 129].clone()
+    a, b = paged.qk_norm_rope(q, k, pos, table, w, w, eps=1e-5, q_out=q, k_out=k)
+    assert a is q and b is k
+    near(q, *want[0])
+    near(k, *want[1])
+    assert torch.equal(x[:, :, 0], edges[0]) and torch.equal(x[:, :, 129], edges[1])
+
+
+def test_qk_norm_rope_many_tokens():
+    """Lane groups that walk several heads, over a head count that they do not divide."""
+    rng = np.random.default_rng(6)
+    q, k = normal(rng, (4099, 37, 16), "bf16"), normal(rng, (4099, 5, 16), "bf16")
+    table = paged.rope_table(4099, 16)
+    pos = torch.arange(4099, dtype=torch.int32, device="cuda").flip(0)
+    w = normal(rng, (16,), "bf16")
+    got = paged.qk_norm_rope(q, k, pos, table, w, w)
+    for x, y in zip((q, k), got):
+        near(y, *sv.norm_rope(f64(x), pos.cpu().numpy(), f64(table), f64(w), 1e-6, "half", "bf16"))
+
+
+def test_positions_outside_the_table_are_nan():
+    rng = np.random.default_rng(7)
+    q = normal(rng, (4, 2, 64), "bf16")
+    table = paged.rope_table(10, 32)
+    pos = torch.tensor([-1, 9, 10, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    got, _ = paged.qk_norm_rope(q, None, pos, table)
+    near(got, *sv.norm_rope(f64(q), pos.cpu().numpy(), f64(table), None, 0, "half", "bf16"))
+    assert torch.isnan(got[[0, 2, 3], :, :32]).all() and not torch.isnan(got[:, :, 32:]).any()
+
+
+# ---- the cache -----------------------------------------------------------------------------------------
+
+def caches(rng, pages, page, kv, dim, dtype, order):
+    if order == "heads":
+        return [normal(rng, (pages, kv, page, dim), dtype).transpose(1, 2) for _ in "kv"]
+    return [normal(rng, (pages, page, kv, dim), dtype) for _ in "kv"]
+
+
+@pytest.mark.parametrize("order", ["heads", "rows"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,kv,dim,rot,layout,norm,page", [
+    (1, 1, 8, 8, "half", False, 1), (1, 8, 128, 128, "half", True, 16), (65, 5, 80, 32, "interleaved", True, 24),
+    (40, 2, 96, 90, "half", True, 7), (300, 2, 256, 0, "half", False, 64), (2100, 8, 64, 64, "half", True, 128)])
+def test_kv_append(order, dtype, tokens, kv, dim, rot, layout, norm, page):
+    rng = np.random.default_rng([tokens, dim, page])
+    pages = -(-tokens // page) + 2
+    kc, vc = caches(rng, pages, page, kv, dim, dtype, order)
+    before = f64(kc), f64(vc)
+    k, v = normal(rng, (tokens, kv, dim), dtype), normal(rng, (tokens, kv + 1, dim), dtype)[:, 1:]
+    slots = rng.permutation(pages * page)[:tokens].astype(np.int64)
+    slots[rng.random(tokens) < 0.2] = -1
+    slots[-1] = pages * page + 3 if tokens > 1 else 0    # past the cache: written nowhere
+    table = positions = None
+    if rot:
+        table = paged.rope_table(4096, rot)
+        positions = torch.from_numpy(rng.integers(0, 4096, tokens).astype(np.int32)).cuda()
+    w = normal(rng, (dim,), dtype) if norm else None
+    paged.kv_append(k, v, kc, vc, torch.from_numpy(slots).cuda(), positions, table, w, layout=layout)
+    args = (positions.cpu().numpy(), f64(table)) if rot else (None, None)
+    ky, kb = sv.norm_rope(f64(k), *args, None if w is None else f64(w), 1e-6, layout, dtype)
+    want = sv.append(*before, ky, f64(v), slots)
+    zero = np.zeros_like(before[0])
+    near(kc, want[0], sv.append(zero, zero, kb, kb, slots)[0])
+    assert np.array_equal(f64(vc), want[1])
+
+
+def test_values_are_copied_bit_for_bit():
+    bits = torch.arange(65536, dtype=torch.int32, device="cuda").to(torch.int16).view(64, 8, 128)
+    v = bits.view(torch.bfloat16)
+    kc, vc = torch.zeros(2, 2, 32, 8, 128, dtype=torch.bfloat16, device="cuda")
+    paged.kv_append(v, v, kc, vc, torch.arange(64, device="cuda").flip(0).contiguous())
+    assert torch.equal(vc.view(torch.int16).view(64, 8, 128).flip(0), bits)
+    assert torch.equal(kc.view(torch.int16), vc.view(torch.int16))   # neither normed nor rotated
+
+
+# ---- attention -------------------------------------------------------------------------------------------
+
+def batch(rng, new, length, heads, kv, dim, dtype, page, order="heads", spare=3, fill=None):
+    """Queries, caches and page lists of sequences with these new and cached tokens.  Rows of pages that no
+    sequence holds are `fill`."""
+    count = [-(-n // page) for n in length]
+    pages = sum(count) + spare
+    kc, vc = caches(rng, pages, page, kv, dim, dtype, order)
+    lists = np.full((len(new), max(count) + 1), -7, np.int32)     # entries nobody reads
+    free = rng.permutation(pages)
+    at = 0
+    held = np.zeros((pages, page), bool)
+    for b, n in enumerate(count):
+        lists[b, :n] = free[at:at + n]
+        for j in range(length[b]):
+            held[lists[b, j // page], j % page] = True
+        at += n
+    if fill is not None:
+        gone = torch.from_numpy(~held).cuda()
+        kc[gone] = fill
+        vc[gone] = fill
+    q = normal(rng, (sum(new), heads, dim), dtype)
+    starts = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+    return q, kc, vc, lists, np.array(length, np.int32), starts
+
+
+def attend(q, kc, vc, lists, lens, starts, **kw):
+    lse = torch.full(q.shape[:2], 7.0, dtype=torch.float32, device="cuda")
+    dev = [torch.from_numpy(x).cuda() for x in (lists, lens, starts)]
+    out = paged.paged_attention(q, kc, vc, *dev, lse=lse, **kw)
+    return out, lse
+
+
+def check(q, kc, vc, lists, lens, starts, dtype, **kw):
+    got = attend(q, kc, vc, lists, lens, starts, **kw)
+    want = sv.attention(f64(q), f64(kc), f64(vc), lists, lens, starts, kw.get("scale"), kw.get("causal", True),
+                        kw.get("window", 0), dtype)
+    near(got[0], want[0], want[2], "out")
+    near(got[1], want[1], want[3], "lse")
+    return got
+
+
+ATTEND = [  # new, length, heads, kv_heads, dim, page
+    ([1], [1], 1, 1, 64, 16),                          # one key
+    ([1], [77], 8, 2, 128, 16),
+    ([1, 1, 1, 1, 1], [5, 0, 300, 129, 64], 4, 4, 64, 7),          # an empty cache among them
+    ([1], [2500], 4, 1, 128, 64),                      # split over workgroups
+    ([1, 1], [3000, 10], 16, 2, 80, 24),               # and beside it one that is not
+    ([3, 0, 40, 1], [3, 0, 170, 65], 6, 2, 96, 5),     # no new tokens; a prompt; a chunk
+    ([33], [33], 1, 1, 8, 1),                          # pages of one row
+    ([70], [1100], 2, 2, 128, 128),                    # rows over two tiles' waves
+    ([130, 7], [130, 1029], 8, 1, 64, 16),
+    ([65], [64], 2, 1, 64, 16),                        # more new tokens than cached: a first row that sees nothing
+    ([12, 5], [0, 3], 4, 2, 72, 16),
+    ([9], [700], 8, 8, 256, 33),
+    ([40], [90], 8, 2, 200, 16),
+    ([300], [2300], 2, 1, 128, 200),                   # a chunk's keys split
+]
+
+
+@pytest.mark.parametrize("order", ["heads", "rows"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new,length,heads,kv,dim,page", ATTEND)
+def test_paged_attention(order, dtype, new, length, heads, kv, dim, page):
+    rng = np.random.default_rng([sum(new), sum(length), dim, page])
+    # what no sequence holds is NaN: rows past a sequence's end among it
+    args = batch(rng, new, length, heads, kv, dim, dtype, page, order, fill=float("nan"))
+    check(*args, dtype, max_q=max(new), max_kv=max(length))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("window", [1, 2, 31, 64, 500, 5000])
+def test_window(dtype, window):
+    rng = np.random.default_rng(window)
+    args = batch(rng, [1, 50, 3, 200], [2000, 60, 3, 1500], 4, 2, 64, dtype, 16, fill=float("nan"))
+    check(*args, dtype, window=window, max_q=200, max_kv=2000)
+    one = batch(rng, [1, 1], [2600, 9], 4, 2, 64, dtype, 16)
+    check(*one, dtype, window=window, max_q=1, max_kv=2600)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_not_causal(dtype):
+    rng = np.random.default_rng(11)
+    args = batch(rng, [40, 1, 7], [100, 900, 3], 4, 2, 128, dtype, 16, fill=float("nan"))
+    check(*args, dtype, causal=False, scale=0.3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hints", [(0, 0), (1, 1), (8, 100), (4096, 1 << 20)])
+def test_hints_do_not_change_what_is_computed(dtype, hints):
+    """Launch sizes too small or too large for the sequences."""
+    rng = np.random.default_rng(12)
+    args = batch(rng, [150, 1, 20], [400, 1500, 20], 8, 2, 64, dtype, 16)
+    check(*args, dtype, max_q=hints[0], max_kv=hints[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_one_token_each_without_starts(dtype):
+    rng = np.random.default_rng(13)
+    q, kc, vc, lists, lens, starts = batch(rng, [1] * 6, [9, 0, 100, 33, 1, 700], 8, 2, 128, dtype, 16)
+    want = attend(q, kc, vc, lists, lens, starts, max_q=1, max_kv=700)
+    lse = torch.empty(6, 8, device="cuda")
+    dev = [torch.from_numpy(x).cuda() for x in (lists, lens)]
+    got = paged.paged_attention(q, kc, vc, *dev, lse=lse, max_kv=700)
+    assert torch.equal(got, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_scores(dtype):
+    """Scores of several hundreds, rising along the keys: the running maximum moves all the time."""
+    rng = np.random.default_rng(14)
+    q, kc, vc, lists, lens, starts = batch(rng, [3, 60], [800, 300], 4, 2, 64, dtype, 16)
+    for b, n in enumerate(lens):
+        for j in range(n):
+            kc[lists[b, j // 16], j % 16] *= 1.0 + j / 16.0
+    check(q, kc, vc, lists, lens, starts, dtype, max_q=60, max_kv=800)
+
+
+def test_strided_queries_and_outputs():
+    rng = np.random.default_rng(15)
+    q, kc, vc, lists, lens, starts = batch(rng, [5, 30], [50, 31], 4, 2, 64, "bf16", 16)
+    packed = torch.zeros(35, 8 * 64, dtype=torch.bfloat16, device="cuda")
+    view = packed[:, 64:5 * 64].view(35, 4, 64)
+    view.copy_(q)
+    want, _ = attend(q, kc, vc, lists, lens, starts)
+    out = torch.zeros(4, 35, 64, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    got, _ = attend(view, kc, vc, lists, lens, starts, out=out)
+    assert got is out and torch.equal(got, want)
+    got, _ = attend(view, kc, vc, lists, lens, starts, out=view)       # in place
+    assert torch.equal(got, want) and not packed[:, :64].any() and not packed[:, 5 * 64:].any()
+
+
+def test_indices_are_brought_into_range():
+    """Lengths and page numbers that leave the arrays: the nearest that do not."""
+    rng = np.random.default_rng(16)
+    q, kc, vc, lists, lens, starts = batch(rng, [4], [60], 2, 2, 64, "f32", 16)
+    odd = lists.copy()
+    odd[0, 0], odd[0, 3:] = -5, 10 ** 6
+    inside = np.clip(odd, 0, kc.shape[0] - 1)
+    over = np.array([10 ** 9], np.int32)                               # all that the list can name
+    got = attend(q, kc, vc, odd, over, starts)
+    want = attend(q, kc, vc, inside, np.array([16 * lists.shape[1]], np.int32), starts)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    none = attend(q, kc, vc, lists, np.array([-3], np.int32), starts)
+    assert not none[0].any() and torch.isneginf(none[1]).all()
+
+
+def test_a_cache_past_32_bit_offsets():
+    """Pages that begin beyond 2^32 bytes and 2^31 values of the cache."""
+    rng = np.random.default_rng(17)
+    page, dim = 4096, 256
+    pages = (2 ** 31) // (page * dim) + 40
+    kc = torch.empty(pages, page, 1, dim, dtype=torch.bfloat16, device="cuda")
+    lists = np.array([[pages - 1, 3, pages - 20]], np.int32)
+    small = normal(rng, (2, 3, page, 1, dim), "bf16")
+    vc = torch.empty_like(kc)
+    k = normal(rng, (9000, 1, dim), "bf16")
+    v = normal(rng, (9000, 1, dim), "bf16")
+    j = np.arange(9000)
+    slots = torch.from_numpy(lists[0].astype(np.int64)[j // page] * page + j % page).cuda()
+    paged.kv_append(k, v, kc, vc, slots)
+    small[0].view(-1, 1, dim)[:9000], small[1].view(-1, 1, dim)[:9000] = k, v
+    q = normal(rng, (2, 4, dim), "bf16")
+    lens, starts = np.array([9000], np.int32), np.array([0, 2], np.int32)
+    got = attend(q, kc, vc, lists, lens, starts)
+    want = attend(q, small[0], small[1], np.array([[0, 1, 2]], np.int32), lens, starts)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    check(q, small[0], small[1], np.array([[0, 1, 2]], np.int32), lens, starts, "bf16")
+
+
+def test_another_stream():
+    rng = np.random.default_rng(18)
+    q, kc, vc, lists, lens, starts = batch(rng, [1], [3000], 8, 2, 128, "bf16", 16)
+    want = attend(q, kc, vc, lists, lens, starts)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        lse = torch.empty(1, 8, device="cuda")
+    dev = [torch.from_numpy(x).cuda() for x in (lists, lens, starts)]
+    torch.cuda.synchronize()
+    out = paged.paged_attention(q, kc, vc, *dev, lse=lse, stream=s)
+    s.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_nothing_to_do():
+    kc = torch.zeros(1, 16, 2, 64, device="cuda")
+    q = torch.zeros(0, 4, 64, device="cuda")
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert paged.paged_attention(q, kc, kc, none.view(0, 3), none).shape == (0, 4, 64)
+    a, b = paged.qk_norm_rope(q, q[:, :2])
+    assert a.shape == q.shape and b.shape == (0, 2, 64)
+    paged.kv_append(q[:, :2], q[:, :2], kc, kc.clone(), none.long())
+    # sequences whose lists name no page
+    one = torch.ones(1, dtype=torch.int32, device="cuda")
+    out = paged.paged_attention(torch.ones(1, 4, 64, device="cuda"), kc, kc, none.view(1, 0), one)
+    assert not out.any()
