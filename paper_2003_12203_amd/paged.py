@@ -21,7 +21,6 @@ slice of a packed projection, a cache that holds a page's heads one after the ot
 from __future__ import annotations
 
 import ctypes as C
-import math
 import struct
 from typing import Optional, Tuple
 
@@ -31,62 +30,49 @@ from . import BF16, DTYPES, F32, FtcnnError, _check, _lib
 
 LAYOUTS = {"half": 0, "interleaved": 1}
 SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
-_DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+_F32, _BF16, _I32, _I64, _U8 = torch.float32, torch.bfloat16, torch.int32, torch.int64, torch.uint8
+_DTYPE = {_F32: F32, _BF16: BF16}
+_CONTIGUOUS = torch.contiguous_format
 
 # the descriptors in the layout of _lib.RopeDesc, AppendDesc and AttentionDesc
 _ROPE = struct.Struct("=9if8q")
 _APPEND = struct.Struct("=10ifi10q")
 _ATTENTION = struct.Struct("=13if11q")
 
+# A decode step makes these calls for every layer and token, so what they cost on the host counts: a
+# tensor's checks are one expression each, and the stream is asked for without a Stream object
+# (0.1 us; torch.cuda.current_stream() 2.7).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+
 
 def _bad(what: str, why: str):
     raise FtcnnError(f"{what}: {why}")
 
 
-def _tensor(what: str, name: str, t: torch.Tensor, dims: int, dtype=None, like: Optional[torch.Tensor] = None):
-    if t.dim() != dims:
-        _bad(what, f"{name} must have {dims} dimensions, not {t.dim()}")
-    if dtype is not None and t.dtype != dtype:
-        _bad(what, f"{name} must be {dtype}, not {t.dtype}")
-    if like is None:
-        if not t.is_cuda:
-            _bad(what, f"{name} must be a device tensor")
-    elif t.device != like.device:
-        _bad(what, f"{name} is on {t.device}, not on {like.device}")
-
-
-def _heads(what: str, name: str, t: torch.Tensor, dims: int, dtype, like):
-    """A tensor of heads: its last dimension contiguous."""
-    _tensor(what, name, t, dims, dtype, like)
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        _bad(what, f"the last dimension of {name} must be contiguous")
-
-
-def _vector(what: str, name: str, t: torch.Tensor, n: int, dtype, like):
-    _tensor(what, name, t, 1, dtype, like)
-    if t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        _bad(what, f"{name} must be a contiguous vector of {n}, not {tuple(t.shape)}")
+def _is(t) -> str:
+    return (f"{t.dtype} {tuple(t.shape)} of strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor)
+            else repr(t))
 
 
 class _On:
-    """The device and stream of a call: allocations and the launch go there."""
+    """The device of a call's tensors and the stream it was given made current: allocations and the launch
+    go there."""
 
     def __init__(self, device: torch.device, stream):
-        self.given = torch.cuda.stream(stream) if stream is not None else None
-        self.device = torch.cuda.device(device) if device.index not in (None, torch.cuda.current_device()) else None
+        self.contexts = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
 
     def __enter__(self):
-        if self.device is not None:
-            self.device.__enter__()
-        if self.given is not None:
-            self.given.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+        for c in self.contexts:
+            c.__enter__()
 
     def __exit__(self, *exc):
-        if self.given is not None:
-            self.given.__exit__(*exc)
-        if self.device is not None:
-            self.device.__exit__(*exc)
+        for c in reversed(self.contexts):
+            c.__exit__(*exc)
+
+
+def _fail(what: str, rc: int):
+    _check(rc, "ftcnn_" + what)
 
 
 def rope_table(max_pos: int, rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
@@ -97,40 +83,41 @@ def rope_table(max_pos: int, rot: int, base: float = 10000.0, scaling: str = "pl
     original, low and high)."""
     if scaling not in SCALINGS:
         _bad("rope_table", f"scaling {scaling!r}: one of {sorted(SCALINGS)}")
-    sc = _lib.RopeScaling(max_pos, rot, SCALINGS[scaling], original, base, factor, low, high, amplitude)
     if not (0 < max_pos < 1 << 31 and 2 <= rot <= 256 and rot % 2 == 0):
         _bad("rope_table", f"max_pos {max_pos}, rot {rot} (even, at most 256)")
-    with _On(torch.device(device), stream) as st:
-        table = torch.empty(max_pos, rot // 2, 2, dtype=torch.float32, device=device)
-        _check(_lib.load().ftcnn_rope_table(C.byref(sc), table.data_ptr(), st), "ftcnn_rope_table")
+    sc = _lib.RopeScaling(max_pos, rot, SCALINGS[scaling], original, base, factor, low, high, amplitude)
+    with _On(torch.device(device), stream):
+        table = torch.empty(max_pos, rot // 2, 2, dtype=_F32, device=device)
+        _fail("rope_table", _lib.load().ftcnn_rope_table(C.byref(sc), table.data_ptr(),
+                                                         torch.cuda.current_stream().cuda_stream))
     return table
 
 
-def _rotation(what, x, positions, table, layout, weights):
-    """(rot, layout, max_pos, weight dtype) of a call on x [tokens][heads][dim]."""
-    if (positions is None) != (table is None):
-        _bad(what, "positions and table go together")
+def _rotation(what, dtype, tokens, dim, dev, positions, table, w0, w1, layout):
+    """(rot, layout, max_pos, weight dtype) of a call on [tokens][heads][dim] of a dtype on device dev."""
     rot = max_pos = 0
     if table is not None:
-        _vector(what, "positions", positions, x.shape[0], torch.int32, x)
-        _tensor(what, "table", table, 3, torch.float32, x)
-        if table.shape[2] != 2 or not table.is_contiguous():
-            _bad(what, f"the table must be a contiguous [max_pos][rot / 2][2], not {tuple(table.shape)}")
-        max_pos, rot = table.shape[0], 2 * table.shape[1]
+        shape = table.shape
+        if not (len(shape) == 3 and shape[2] == 2 and table.dtype is _F32 and table.is_contiguous() and
+                table.get_device() == dev):
+            _bad(what, f"the table must be a contiguous float32 [max_pos][rot / 2][2] on device {dev}, not {_is(table)}")
+        if positions is None or not (positions.dtype is _I32 and positions.shape == (tokens,) and
+                                     positions.is_contiguous() and positions.get_device() == dev):
+            _bad(what, f"positions must be a contiguous int32 [{tokens}] on device {dev}, not {_is(positions)}")
+        max_pos, rot = shape[0], 2 * shape[1]
+    elif positions is not None:
+        _bad(what, "positions need a table")
     if layout not in LAYOUTS:
         _bad(what, f"layout {layout!r}: one of {sorted(LAYOUTS)}")
     wd = None
-    for w in weights:
+    for w in (w0, w1):
         if w is not None:
-            _vector(what, "a weight", w, x.shape[2], None, x)
-            if w.dtype not in (torch.float32, x.dtype) or (wd is not None and w.dtype != wd):
-                _bad(what, f"weights must be float32 or {x.dtype}, both the same")
+            if not (w.shape == (dim,) and w.is_contiguous() and w.get_device() == dev and
+                    (w.dtype is dtype or w.dtype is _F32) and (wd is None or wd is w.dtype)):
+                _bad(what, f"weights must be contiguous [{dim}] of float32 or {dtype}, both alike, on device {dev}, "
+                           f"not {_is(w)}")
             wd = w.dtype
     return rot, LAYOUTS[layout], max_pos, F32 if wd is None else _DTYPE[wd]
-
-
-def _at(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
 
 
 def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
@@ -145,47 +132,50 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     x = q if q is not None else k
     if x is None:
         _bad(what, "neither queries nor keys")
-    if x.dtype not in _DTYPE:
-        _bad(what, f"dtype {x.dtype}")
-    for name, t in (("q", q), ("k", k)):
-        if t is not None:
-            _heads(what, name, t, 3, x.dtype, None if t is x else x)
-            if t.shape[0] != x.shape[0] or t.shape[2] != x.shape[2]:
-                _bad(what, "q and k must agree on tokens and dim")
-    rot, lay, max_pos, wd = _rotation(what, x, positions, table, layout, (q_weight, k_weight))
-    tokens, _, dim = x.shape
-    with _On(x.device, stream) as st:
-        outs, hd, si, so = [], [], [], []
-        for name, t, o in (("q_out", q, q_out), ("k_out", k, k_out)):
-            if t is None:
-                outs.append(None)
-                hd.append(0)
-                si += (0, 0)
-                so += (0, 0)
-                continue
-            if o is None:
-                o = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-            else:
-                _heads(what, name, o, 3, t.dtype, x)
-                if o.shape != t.shape:
-                    _bad(what, f"{name} must be {tuple(t.shape)}, not {tuple(o.shape)}")
-            outs.append(o)
-            hd.append(t.shape[1])
-            si += t.stride()[:2]
-            so += o.stride()[:2]
-        desc = _ROPE.pack(_DTYPE[x.dtype], tokens, hd[0], hd[1], dim, rot, lay, max_pos, wd, eps, *si, *so)
-        _check(_lib.load().ftcnn_qk_norm_rope(desc, _at(q), _at(k), _at(positions), _at(table), _at(q_weight),
-                                              _at(k_weight), _at(outs[0]), _at(outs[1]), st), "ftcnn_qk_norm_rope")
-    return outs[0], outs[1]
-
-
-def _caches(what, k_cache, v_cache, like, kv_heads, dim):
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _heads(what, name, t, 4, like.dtype, like)
-    shape = k_cache.shape
-    if v_cache.shape != shape or shape[3] != dim or (kv_heads is not None and shape[2] != kv_heads):
-        _bad(what, f"caches of {tuple(shape)} and {tuple(v_cache.shape)} for heads of {dim}")
-    return shape
+    dtype, shape, dev = x.dtype, x.shape, x.get_device()
+    if dtype not in _DTYPE or len(shape) != 3 or dev < 0:
+        _bad(what, f"queries and keys are float32 or bfloat16 [tokens][heads][dim] on a device, not {_is(x)}")
+    if stream is not None or dev != _current_device():
+        with _On(x.device, stream):
+            return qk_norm_rope(q, k, positions, table, q_weight, k_weight, eps, layout, q_out, k_out)
+    tokens, heads, dim = shape
+    kv_heads = 0
+    rot, lay, max_pos, wd = _rotation(what, dtype, tokens, dim, dev, positions, table, q_weight, k_weight, layout)
+    qi = qo = ki = ko = (0, 0, 1)
+    if q is None:
+        heads, q_out = 0, None
+    else:
+        qi = q.stride()
+        if q_out is None:
+            q_out = torch.empty_like(q, memory_format=_CONTIGUOUS)
+        elif not (q_out.dtype is dtype and q_out.shape == shape and q_out.get_device() == dev):
+            _bad(what, f"q_out must be like q, not {_is(q_out)}")
+        qo = q_out.stride()
+    if k is None:
+        k_out = None
+    else:
+        ki, kshape = k.stride(), k.shape
+        if not (k.dtype is dtype and len(kshape) == 3 and kshape[0] == tokens and kshape[2] == dim and
+                k.get_device() == dev):
+            _bad(what, f"k must be {dtype} [{tokens}][kv_heads][{dim}] on device {dev}, not {_is(k)}")
+        kv_heads = kshape[1]
+        if k_out is None:
+            k_out = torch.empty_like(k, memory_format=_CONTIGUOUS)
+        elif not (k_out.dtype is dtype and k_out.shape == kshape and k_out.get_device() == dev):
+            _bad(what, f"k_out must be like k, not {_is(k_out)}")
+        ko = k_out.stride()
+    if not qi[2] == qo[2] == ki[2] == ko[2] == 1:
+        _bad(what, "the last dimension of queries, keys and outputs must be contiguous")
+    desc = _ROPE.pack(_DTYPE[dtype], tokens, heads, kv_heads, dim, rot, lay, max_pos, wd, eps, qi[0], qi[1], ki[0],
+                      ki[1], qo[0], qo[1], ko[0], ko[1])
+    rc = _lib.load().ftcnn_qk_norm_rope(
+        desc, None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
+        None if positions is None else positions.data_ptr(), None if table is None else table.data_ptr(),
+        None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+        None if q is None else q_out.data_ptr(), None if k is None else k_out.data_ptr(), _raw_stream(dev))
+    if rc:
+        _fail(what, rc)
+    return q_out, k_out
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor,
@@ -195,21 +185,35 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: 
     """ftcnn_kv_append: the new tokens' keys (normed with a weight, rotated with positions and a table) and
     values into the cache rows slots (int64 [tokens], page * rows of a page + row; -1: nowhere)."""
     what = "kv_append"
-    if k.dtype not in _DTYPE:
-        _bad(what, f"dtype {k.dtype}")
-    _heads(what, "k", k, 3, None, None)
-    _heads(what, "v", v, 3, k.dtype, k)
-    if v.shape != k.shape:
-        _bad(what, f"k {tuple(k.shape)} and v {tuple(v.shape)} must agree")
-    tokens, kv_heads, dim = k.shape
-    pages, page = _caches(what, k_cache, v_cache, k, kv_heads, dim)[:2]
-    _vector(what, "slots", slots, tokens, torch.int64, k)
-    rot, lay, max_pos, wd = _rotation(what, k, positions, table, layout, (k_weight,))
-    with _On(k.device, stream) as st:
-        desc = _APPEND.pack(_DTYPE[k.dtype], tokens, kv_heads, dim, rot, lay, max_pos, wd, pages, page, eps, 0,
-                            *k.stride()[:2], *v.stride()[:2], *k_cache.stride()[:3], *v_cache.stride()[:3])
-        _check(_lib.load().ftcnn_kv_append(desc, _at(k), _at(v), _at(positions), _at(table), _at(k_weight),
-                                           _at(slots), _at(k_cache), _at(v_cache), st), "ftcnn_kv_append")
+    dtype, shape, dev = k.dtype, k.shape, k.get_device()
+    if dtype not in _DTYPE or len(shape) != 3 or dev < 0:
+        _bad(what, f"keys are float32 or bfloat16 [tokens][kv_heads][dim] on a device, not {_is(k)}")
+    if stream is not None or dev != _current_device():
+        with _On(k.device, stream):
+            return kv_append(k, v, k_cache, v_cache, slots, positions, table, k_weight, eps, layout)
+    tokens, kv_heads, dim = shape
+    if not (v.dtype is dtype and v.shape == shape and v.get_device() == dev):
+        _bad(what, f"v must be like k, {dtype} {tuple(shape)} on device {dev}, not {_is(v)}")
+    cache = k_cache.shape
+    if not (k_cache.dtype is dtype and len(cache) == 4 and cache[2] == kv_heads and cache[3] == dim and
+            k_cache.get_device() == dev):
+        _bad(what, f"k_cache must be {dtype} [pages][page][{kv_heads}][{dim}] on device {dev}, not {_is(k_cache)}")
+    if not (v_cache.dtype is dtype and v_cache.shape == cache and v_cache.get_device() == dev):
+        _bad(what, f"v_cache must be like k_cache, {dtype} {tuple(cache)} on device {dev}, not {_is(v_cache)}")
+    if not (slots.dtype is _I64 and slots.shape == (tokens,) and slots.is_contiguous() and slots.get_device() == dev):
+        _bad(what, f"slots must be a contiguous int64 [{tokens}] on device {dev}, not {_is(slots)}")
+    rot, lay, max_pos, wd = _rotation(what, dtype, tokens, dim, dev, positions, table, k_weight, None, layout)
+    ks, vs, kc, vc = k.stride(), v.stride(), k_cache.stride(), v_cache.stride()
+    if not ks[2] == vs[2] == kc[3] == vc[3] == 1:
+        _bad(what, "the last dimension of keys, values and caches must be contiguous")
+    desc = _APPEND.pack(_DTYPE[dtype], tokens, kv_heads, dim, rot, lay, max_pos, wd, cache[0], cache[1], eps, 0,
+                        ks[0], ks[1], vs[0], vs[1], kc[0], kc[1], kc[2], vc[0], vc[1], vc[2])
+    rc = _lib.load().ftcnn_kv_append(
+        desc, k.data_ptr(), v.data_ptr(), None if positions is None else positions.data_ptr(),
+        None if table is None else table.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+        slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _raw_stream(dev))
+    if rc:
+        _fail(what, rc)
 
 
 def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_list: torch.Tensor,
@@ -221,48 +225,62 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     pages (page_list int32 [batch][entries], kv_lens int32 [batch], the new tokens' rows among them).
     q_starts int32 [batch + 1] says whose tokens are whose (None: one of each sequence).  max_q and max_kv, the
     longest sequence's new and cached tokens where the caller knows them, size the launch.  scale defaults to
-    1 / sqrt(dim).  lse (float32 [tokens][heads]) is filled when given.  workspace: uint8, 256-byte aligned,
-    of attention_workspace_bytes; allocated when needed and not given."""
+    1 / sqrt(dim).  lse (float32 [tokens][heads]) is filled when given.  workspace: uint8, 256-byte aligned;
+    allocated when needed and not given."""
     what = "paged_attention"
-    if q.dtype not in _DTYPE:
-        _bad(what, f"dtype {q.dtype}")
-    _heads(what, "q", q, 3, None, None)
-    tokens, heads, dim = q.shape
-    pages, page, kv_heads, _ = _caches(what, k_cache, v_cache, q, None, dim)
-    _tensor(what, "page_list", page_list, 2, torch.int32, q)
-    batch, entries = page_list.shape
-    if entries > 1 and page_list.stride(1) != 1:
-        _bad(what, "the last dimension of page_list must be contiguous")
-    _vector(what, "kv_lens", kv_lens, batch, torch.int32, q)
-    if q_starts is not None:
-        _vector(what, "q_starts", q_starts, batch + 1, torch.int32, q)
-    if lse is not None:
-        _tensor(what, "lse", lse, 2, torch.float32, q)
-        if lse.shape != q.shape[:2] or not lse.is_contiguous():
-            _bad(what, f"lse must be a contiguous {tuple(q.shape[:2])}")
-    if out is not None:
-        _heads(what, "out", out, 3, q.dtype, q)
-        if out.shape != q.shape:
-            _bad(what, f"out must be {tuple(q.shape)}, not {tuple(out.shape)}")
-    with _On(q.device, stream) as st:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        desc = _ATTENTION.pack(_DTYPE[q.dtype], batch, tokens, heads, kv_heads, dim, pages, page, entries,
-                               int(causal), window, max_q, max_kv, 1.0 / math.sqrt(dim) if scale is None else scale,
-                               *q.stride()[:2], *out.stride()[:2], *k_cache.stride()[:3], *v_cache.stride()[:3],
-                               page_list.stride(0))
-        L = _lib.load()
-        need = L.ftcnn_paged_attention_workspace_bytes(desc)
-        if need:
-            if workspace is None:
-                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            else:
-                _tensor(what, "workspace", workspace, 1, torch.uint8, q)
-                if workspace.numel() < need or not workspace.is_contiguous():
-                    _bad(what, f"the workspace must be {need} contiguous bytes, not {workspace.numel()}")
-        _check(L.ftcnn_paged_attention(desc, _at(q), _at(k_cache), _at(v_cache), _at(page_list), _at(kv_lens),
-                                       _at(q_starts), _at(out), _at(lse), _at(workspace) if need else None, st),
-               "ftcnn_paged_attention")
+    dtype, shape, dev = q.dtype, q.shape, q.get_device()
+    if dtype not in _DTYPE or len(shape) != 3 or dev < 0:
+        _bad(what, f"queries are float32 or bfloat16 [tokens][heads][dim] on a device, not {_is(q)}")
+    if stream is not None or dev != _current_device():
+        with _On(q.device, stream):
+            return paged_attention(q, k_cache, v_cache, page_list, kv_lens, q_starts, max_q, max_kv, scale, causal,
+                                   window, out, lse, workspace)
+    tokens, heads, dim = shape
+    cache = k_cache.shape
+    if not (k_cache.dtype is dtype and len(cache) == 4 and cache[3] == dim and k_cache.get_device() == dev):
+        _bad(what, f"k_cache must be {dtype} [pages][page][kv_heads][{dim}] on device {dev}, not {_is(k_cache)}")
+    if not (v_cache.dtype is dtype and v_cache.shape == cache and v_cache.get_device() == dev):
+        _bad(what, f"v_cache must be like k_cache, {dtype} {tuple(cache)} on device {dev}, not {_is(v_cache)}")
+    lists = page_list.shape
+    if not (page_list.dtype is _I32 and len(lists) == 2 and (page_list.stride(1) == 1 or lists[1] < 2) and
+            page_list.get_device() == dev):
+        _bad(what, f"page_list must be int32 [batch][entries], entries contiguous, on device {dev}, not "
+                   f"{_is(page_list)}")
+    batch, entries = lists
+    if not (kv_lens.dtype is _I32 and kv_lens.shape == (batch,) and kv_lens.is_contiguous() and
+            kv_lens.get_device() == dev):
+        _bad(what, f"kv_lens must be a contiguous int32 [{batch}] on device {dev}, not {_is(kv_lens)}")
+    if q_starts is not None and not (q_starts.dtype is _I32 and q_starts.shape == (batch + 1,) and
+                                     q_starts.is_contiguous() and q_starts.get_device() == dev):
+        _bad(what, f"q_starts must be a contiguous int32 [{batch + 1}] on device {dev}, not {_is(q_starts)}")
+    if lse is not None and not (lse.dtype is _F32 and lse.shape == (tokens, heads) and lse.is_contiguous() and
+                                lse.get_device() == dev):
+        _bad(what, f"lse must be a contiguous float32 [{tokens}][{heads}] on device {dev}, not {_is(lse)}")
+    if out is None:
+        out = torch.empty_like(q, memory_format=_CONTIGUOUS)
+    elif not (out.dtype is dtype and out.shape == shape and out.get_device() == dev):
+        _bad(what, f"out must be like q, {dtype} {tuple(shape)} on device {dev}, not {_is(out)}")
+    qs, os, kc, vc = q.stride(), out.stride(), k_cache.stride(), v_cache.stride()
+    if not qs[2] == os[2] == kc[3] == vc[3] == 1:
+        _bad(what, "the last dimension of queries, caches and outputs must be contiguous")
+    desc = _ATTENTION.pack(_DTYPE[dtype], batch, tokens, heads, cache[2], dim, cache[0], cache[1], entries, causal,
+                           window, max_q, max_kv, dim ** -0.5 if scale is None else scale, qs[0], qs[1], os[0], os[1],
+                           kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], page_list.stride(0))
+    L = _lib.load()
+    need = L.ftcnn_paged_attention_workspace_bytes(desc)
+    room = None
+    if need:
+        if workspace is None:
+            workspace = torch.empty(need, dtype=_U8, device=q.device)
+        elif not (workspace.dtype is _U8 and workspace.numel() >= need and workspace.is_contiguous() and
+                  workspace.get_device() == dev):
+            _bad(what, f"the workspace must be {need} contiguous bytes on device {dev}, not {_is(workspace)}")
+        room = workspace.data_ptr()
+    rc = L.ftcnn_paged_attention(desc, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), page_list.data_ptr(),
+                                 kv_lens.data_ptr(), None if q_starts is None else q_starts.data_ptr(),
+                                 out.data_ptr(), None if lse is None else lse.data_ptr(), room, _raw_stream(dev))
+    if rc:
+        _fail(what, rc)
     return out
 
 
