@@ -23,8 +23,9 @@ inline FastDiv fast_div(uint32_t d) {
     }
     return f;
 }
+__device__ inline uint32_t div_by_many(uint32_t n, const FastDiv &f) { return __umulhi(n, f.mul) >> f.shift; }   // d > 1
 __device__ inline uint32_t div_by(uint32_t n, const FastDiv &f) {
-    return f.d > 1 ? __umulhi(n, f.mul) >> f.shift : n;
+    return f.d > 1 ? div_by_many(n, f) : n;
 }
 
 struct RopeArgs {
@@ -48,27 +49,40 @@ hipError_t launch_rope_table(const ftcnn_rope_scaling &sc, float *table, hipStre
 // Units (two vectors of values) of a row, and lanes of a group, that the launch takes for its arguments
 hipError_t launch_rope(int dtype, RopeArgs a, bool aligned, hipStream_t st);
 
+// A unit that a run of key tiles starts inside of: the first and last run that hold some of it (first_run
+// < 0: the run starts with a unit, or is empty), the first row of its sequence's queries, its key head,
+// first row of the sequence's rows and count of rows.
+struct AttnCut {
+    int first_run, last_run, q0, head, r0, rows;
+};
+
 struct AttnArgs {
     const void *q, *k, *v;
     void *o;
     float *lse, *part_o, *part_ml;
+    AttnCut *cuts;
     const int32_t *page_list, *kv_lens, *q_starts;
-    long long qs[2], os[2], ks[3], vs[3];   // elements: token, head; page, row, head
+    long long qs[2], os[2];      // elements: token, head
+    unsigned kb[3], vb[3];       // bytes: page, row, head
     long long list_stride;
     int batch, tokens, kv_heads, group, dim;
     int pages, page, capacity;   // pages of the cache, rows of a page, rows a page list can name
     int causal, window;
-    int tiles, splits, per_split;
-    int interleave;              // workgroup order: pairs of (sequence, key head) dealt to the eight XCDs
+    int tiles;                   // whole units: row tiles that the launch has for a sequence
+    int groups, min_run;         // even runs (groups > 0): workgroups, and keys that a run has at least
+    int unit_cost;               // ... and what the start of a unit counts, in keys
+    int tile_keys;
+    int part_rows;               // rows of a part in the workspace
+    int interleave;              // whole units: pairs of (sequence, key head) dealt to the eight XCDs
     FastDiv div_page, div_group;
     float scale_log2;            // scale * log2(e): the softmax in powers of two
 };
-// What a call launches: rows of a workgroup's tile, and how far the cached tokens are split.
+// What a call launches.
 struct AttnPlan {
     int dp;                      // head size the kernel is compiled for
-    int wr, wk;                  // waves along the rows of 32, and along the keys
-    int tiles, splits, per_split;
-    size_t part_o, bytes;        // workspace: the splits' outputs, then their maxima and sums
+    int rows, keys;              // of a unit's tiles: 16 or 32 rows: stream_kernel, more: attn_kernel
+    int tiles, groups, min_run, unit_cost, part_rows, join_rows;
+    size_t part_ml, cuts, bytes;   // workspace: the parts' outputs, their maxima and sums, the cuts
 };
 AttnPlan attn_plan(const ftcnn_attention_desc &d);
 hipError_t launch_attn_bf16(const AttnPlan &pl, const AttnArgs &a, hipStream_t st);

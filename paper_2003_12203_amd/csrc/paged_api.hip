@@ -58,29 +58,38 @@ AttnPlan attn_plan(const ftcnn_attention_desc &d) {
     const long long max_kv = std::max(1LL, std::min(d.max_kv > 0 ? d.max_kv : capacity, capacity));
     const long long rows = max_q * group;
     p.dp = d.dim <= 64 ? 64 : (d.dim <= 128 ? 128 : 256);
-    if (d.dtype == FTCNN_F32) {
-        p.wr = rows <= 32 ? 1 : 4;
-        p.wk = p.wr > 1 ? 1 : (p.dp > 128 ? 1 : (p.dp > 64 ? 2 : 4));
-    } else {
-        p.wr = rows <= 32 ? 1 : (rows <= 64 ? 2 : (p.dp > 128 ? 4 : 8));
-        p.wk = p.wr > 2 ? 1 : (p.wr == 2 ? 2 : (p.dp > 128 ? 2 : 4));
-    }
-    const long long tile = 32 * p.wr;
+    const bool bf = d.dtype == FTCNN_BF16;
+    const long long es = bf ? 2 : 4;
+    if (rows <= 32) p.rows = rows <= 16 ? 16 : 32;
+    else if (!bf) p.rows = 128;
+    else p.rows = rows <= 64 ? 64 : 128;
+    if (p.rows <= 32) p.keys = p.dp * es <= 256 ? 32 : 16;
+    else p.keys = bf && p.dp <= 128 && p.rows == 128 ? 64 : 32;
+    const long long tile = p.rows;
     p.tiles = (int)((rows + tile - 1) / tile);
+    // workgroups that are on the device at a time
+    long long fit;
+    if (tile <= 32) {
+        fit = kComputeUnits * (p.dp * es * tile <= 4096 ? 8 : 4);
+    } else {
+        const long long lds = 4LL * p.keys * p.dp * es;
+        fit = kComputeUnits * std::max(1LL, std::min<long long>((kUnitLds - 1) / lds, 256 / tile));
+    }
     const long long some = std::min<long long>((long long)d.batch * p.tiles, d.tokens * group / tile + d.batch);
-    const long long groups = std::max(1LL, some * d.kv_heads);
-    const long long range = d.window > 0 ? std::min<long long>(max_kv, (long long)d.window + tile / group + 1) : max_kv;
-    const long long want = (512 + groups - 1) / groups;
-    long long per = (range + want - 1) / want;
-    per = std::max<long long>(per, p.wr > 2 ? 1024 : 512);
-    if (p.wr <= 2) per = std::min<long long>(per, 2048);
-    per = (per + 127) / 128 * 128;
-    p.splits = (int)((range + per - 1) / per);
-    p.per_split = (int)per;
-    if (p.splits > 1) {
-        const size_t n = (size_t)d.tokens * d.heads * p.splits;
-        p.part_o = (n * d.dim * sizeof(float) + 255) & ~size_t(255);
-        p.bytes = p.part_o + ((n * 2 * sizeof(float) + 255) & ~size_t(255));
+    const long long units = some * d.kv_heads;
+    const long long range = d.window > 0 ? std::min<long long>(max_kv, d.window + tile / group + 1) : max_kv;
+    p.min_run = 8 * p.keys;
+    p.unit_cost = (p.rows <= 32 ? 1 : 3) * p.keys;
+    bool even = range > p.min_run && units < 4 * fit;
+    if (even) {
+        p.groups = (int)std::min(fit, (units * range + p.min_run - 1) / p.min_run);
+        p.part_rows = (int)std::min<long long>(tile, d.tokens * group);
+        p.join_rows = tile > 32 ? 8 : (p.groups >= 32 * units ? 1 : 32);
+        const size_t n = 2 * (size_t)p.groups * p.part_rows;
+        auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
+        p.part_ml = up(n * d.dim * sizeof(float));
+        p.cuts = p.part_ml + up(n * 2 * sizeof(float));
+        p.bytes = p.cuts + up(p.groups * sizeof(AttnCut));
     }
     return p;
 }
@@ -245,13 +254,16 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
     for (int i = 0; i < 3; ++i) {
         if (i < 2) al = al && d->q_stride[i] % vec == 0 && d->out_stride[i] % vec == 0;
         al = al && d->k_cache_stride[i] % vec == 0 && d->v_cache_stride[i] % vec == 0;
+        if (std::min(d->k_cache_stride[i], d->v_cache_stride[i]) < 0 ||
+            std::max(d->k_cache_stride[i], d->v_cache_stride[i]) > kMaxRows / 2)
+            return set_error(FTCNN_E_UNSUPPORTED, "%s: cache strides are 0 to 2^29 elements", what);
     }
     if (!al)
         return set_error(FTCNN_E_UNSUPPORTED, "%s: rows of q, out and the cache must start on 16 bytes", what);
     const AttnPlan pl = attn_plan(*d);
     if (pl.bytes && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256))
         return set_error(FTCNN_E_WORKSPACE, "%s: workspace missing or not 256-byte aligned", what);
-    const long long blocks = (long long)pl.tiles * pl.splits * d->kv_heads * d->batch;
+    const long long blocks = pl.groups ? pl.groups : (long long)pl.tiles * d->kv_heads * d->batch;
     if (blocks > 0x7fffffffLL) return set_error(FTCNN_E_SHAPE, "%s: %lld workgroups", what, blocks);
     AttnArgs a{};
     a.q = q;
@@ -259,8 +271,12 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
     a.v = v_cache;
     a.o = out;
     a.lse = lse;
-    a.part_o = static_cast<float *>(workspace);
-    a.part_ml = workspace ? reinterpret_cast<float *>(static_cast<char *>(workspace) + pl.part_o) : nullptr;
+    if (pl.bytes) {
+        char *ws = static_cast<char *>(workspace);
+        a.part_o = reinterpret_cast<float *>(ws);
+        a.part_ml = reinterpret_cast<float *>(ws + pl.part_ml);
+        a.cuts = reinterpret_cast<AttnCut *>(ws + pl.cuts);
+    }
     a.page_list = page_list;
     a.kv_lens = kv_lens;
     a.q_starts = q_starts;
@@ -269,8 +285,8 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
             a.qs[i] = d->q_stride[i];
             a.os[i] = d->out_stride[i];
         }
-        a.ks[i] = d->k_cache_stride[i];
-        a.vs[i] = d->v_cache_stride[i];
+        a.kb[i] = (unsigned)(d->k_cache_stride[i] * (16 / vec));
+        a.vb[i] = (unsigned)(d->v_cache_stride[i] * (16 / vec));
     }
     a.list_stride = d->list_stride;
     a.batch = d->batch;
@@ -284,14 +300,17 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
     a.causal = d->causal != 0;
     a.window = d->window;
     a.tiles = pl.tiles;
-    a.splits = pl.splits;
-    a.per_split = pl.per_split;
+    a.groups = pl.groups;
+    a.min_run = pl.min_run;
+    a.unit_cost = pl.unit_cost;
+    a.tile_keys = pl.keys;
+    a.part_rows = pl.part_rows;
     a.interleave = pl.tiles > 1 && (long long)d->batch * d->kv_heads % 8 == 0;
     a.div_page = fast_div((uint32_t)d->page);
     a.div_group = fast_div((uint32_t)a.group);
     a.scale_log2 = d->scale * 1.44269504088896340736f;
     FT_PAGED_HIP(d->dtype == FTCNN_F32 ? launch_attn_f32(pl, a, stream) : launch_attn_bf16(pl, a, stream), what);
-    if (pl.splits > 1) FT_PAGED_HIP(launch_attn_join(d->dtype, pl, a, stream), "paged_attention: join");
+    if (pl.groups) FT_PAGED_HIP(launch_attn_join(d->dtype, pl, a, stream), "paged_attention: join");
     return FTCNN_OK;
 }
 

@@ -1,13 +1,13 @@
 // bf16 instances of the attention kernel.
-#include "paged_attn.h"
+#include "paged_stream.h"
 
 namespace ftcnn {
 namespace {
 template <int DP> hipError_t pick(const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
-    constexpr bool wide = DP > 128;
-    if (pl.wr == 1) return attn_go<uint16_t, DP, 1, wide ? 2 : 4, 1>(a, st);
-    if (pl.wr == 2) return attn_go<uint16_t, DP, 2, 2, 1>(a, st);
-    return attn_go<uint16_t, DP, wide ? 4 : 8, 1, wide ? 1 : 2>(a, st);
+    if (pl.rows == 16) return stream_go<uint16_t, DP, 1>(a, st);
+    if (pl.rows == 32) return stream_go<uint16_t, DP, 2>(a, st);
+    if (pl.rows == 64) return attn_go<uint16_t, DP, 2, 1>(a, st);
+    return attn_go<uint16_t, DP, 4, (DP <= 128 ? 2 : 1)>(a, st);
 }
 }  // namespace
 

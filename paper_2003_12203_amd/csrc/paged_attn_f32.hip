@@ -1,12 +1,12 @@
 // fp32 instances of the attention kernel.
-#include "paged_attn.h"
+#include "paged_stream.h"
 
 namespace ftcnn {
 namespace {
 template <int DP> hipError_t pick(const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
-    constexpr int WK = DP == 64 ? 4 : (DP == 128 ? 2 : 1);
-    if (pl.wr == 1) return attn_go<float, DP, 1, WK, 1>(a, st);
-    return attn_go<float, DP, 4, 1, 1>(a, st);
+    if (pl.rows == 16) return stream_go<float, DP, 1>(a, st);
+    if (pl.rows == 32) return stream_go<float, DP, 2>(a, st);
+    return attn_go<float, DP, 4, 1>(a, st);
 }
 }  // namespace
 

@@ -1,89 +1,126 @@
-// Joins the outputs of the splits of a row's keys: with each split's maximum m_s (in powers of two),
-// sum l_s and unnormalised output o_s, O = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s with
-// M = max_s m_s, in the order of the splits.  One workgroup a row; its waves' halves take the splits in
-// turn, 16 bytes a lane.
+// Joins the parts of a unit whose keys several workgroups walked: with each part's maximum m_s (in powers
+// of two), sum l_s and unnormalised output o_s of a row,
+//   O = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s,  M = max_s m_s,
+// in an order that the parts' count and place alone decide.  The run that a unit's second part lies in says
+// what there is to join (AttnCut).  A workgroup looks through some of the runs and takes some of each such
+// unit's rows: a team of 32 lanes (four values a lane) a row, or with fewer rows than teams several that
+// share a row's parts.
+#include <algorithm>
+
 #include "paged_attn.h"
 
 namespace ftcnn {
 namespace {
 
-template <typename T, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void attn_join_kernel(AttnArgs a, int rows_tile) {
-    constexpr int TEAMS = 2 * WAVES;   // 32 lanes each: a split's values, four a lane, in up to two steps
-    __shared__ float part[TEAMS][256];
-    const int heads = a.kv_heads * a.group;
-    const int token = blockIdx.x / heads, head = blockIdx.x % heads;
-    const int lane = threadIdx.x & 31, team = threadIdx.x >> 5;
-    // the sequence of this token: the last that starts at or before it and is not empty
-    int b = token;
-    if (a.q_starts) {
-        int lo = 0, hi = a.batch;   // starts[lo] <= token < starts[hi], should there be such
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (a.q_starts[mid] <= token) lo = mid;
-            else hi = mid;
-        }
-        b = lo;
-    }
-    int q0, nq, kv;
-    attn_sequence(a, b, q0, nq, kv);
-    if (token < q0 || token >= q0 + nq) return;   // nobody's token
-    const int first = (token - q0) * a.group + head % a.group;   // its row
-    const int r0 = first / rows_tile * rows_tile;
-    const int i0 = r0 / a.group, i1 = (min(r0 + rows_tile, nq * a.group) - 1) / a.group;
-    int k0, k1;
-    const int used = attn_range(a, nq, kv, i0, i1, 0, k0, k1);
-    if (used == 1) return;   // the attention kernel wrote it
-    const long long orow = blockIdx.x;
-    const float *ml = a.part_ml + orow * a.splits * 2, *po = a.part_o + orow * a.splits * a.dim;
-    float top = -INFINITY;
-    for (int s = threadIdx.x & 63; s < used; s += 64) top = fmaxf(top, ml[2 * s]);
-#pragma unroll
-    for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
-    const float mt = top == -INFINITY ? 0.0f : top;
-    float l = 0.0f;
-    for (int s = threadIdx.x & 63; s < used; s += 64) l += ml[2 * s + 1] * __builtin_amdgcn_exp2f(ml[2 * s] - mt);
-#pragma unroll
-    for (int x = 32; x > 0; x /= 2) l += __shfl_xor(l, x);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    for (int d0 = 0; d0 < a.dim; d0 += 128) {
-        const int d = d0 + lane * 4;
-        if (d < a.dim) {
-            float4 acc = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-            for (int s = team; s < used; s += TEAMS) {
-                const float wgt = __builtin_amdgcn_exp2f(ml[2 * s] - mt);
-                const float4 v = *reinterpret_cast<const float4 *>(po + (long long)s * a.dim + d);
-                acc.x = fmaf(wgt, v.x, acc.x);
-                acc.y = fmaf(wgt, v.y, acc.y);
-                acc.z = fmaf(wgt, v.z, acc.z);
-                acc.w = fmaf(wgt, v.w, acc.w);
-            }
-            *reinterpret_cast<float4 *>(&part[team][d]) = acc;
-        }
-    }
-    __syncthreads();
-    T *out = static_cast<T *>(a.o) + (long long)token * a.os[0] + (long long)head * a.os[1];
-    for (int d = threadIdx.x; d < a.dim; d += 64 * WAVES) {
-        float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < TEAMS; ++k) sum += part[k][d];
-        Elem<T>::store(out, d, sum * inv);
-    }
-    if (a.lse && threadIdx.x == 0) a.lse[orow] = l == 0.0f ? -INFINITY : (mt + __log2f(l)) * 0.693147180559945309f;
-}
+constexpr int kTeams = kThreads / 32;
 
-template <typename T> hipError_t go(const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
-    const unsigned rows = (unsigned)(a.tokens * a.kv_heads * a.group);
-    if (a.splits <= 8) attn_join_kernel<T, 1><<<rows, 64, 0, st>>>(a, pl.wr * 32);
-    else attn_join_kernel<T, 4><<<rows, 256, 0, st>>>(a, pl.wr * 32);
-    return hipGetLastError();
+template <typename T>
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, int rows_here) {
+    __shared__ float4 sums[kTeams][64];
+    const int lane = threadIdx.x & 31, team = threadIdx.x >> 5;
+    const int wave_lane = threadIdx.x & 63;
+    for (int c0 = blockIdx.x; c0 < a.groups; c0 += 64 * gridDim.x) {
+        // the runs of this workgroup that a unit's second part lies in
+        const long long mine = c0 + (long long)wave_lane * gridDim.x;
+        unsigned long long owned = __ballot(mine < a.groups && a.cuts[min(mine, a.groups - 1LL)].first_run == mine - 1 &&
+                                            mine > 0);
+        for (; owned; owned &= owned - 1) {
+            const AttnCut cut = a.cuts[c0 + __builtin_ctzll(owned) * gridDim.x];
+            const int from = blockIdx.y * rows_here, rows = min(cut.rows - from, rows_here);
+            if (rows <= 0) continue;
+            const int parts = cut.last_run - cut.first_run + 1;
+            const int share = rows >= kTeams ? 1 : (rows > 4 ? 1 : (rows > 2 ? 2 : (rows > 1 ? 4 : 8)));   // teams a row
+            const int sub = team % share;
+            for (int r0 = 0; r0 < rows; r0 += kTeams / share) {
+                const int row = from + r0 + team / share;
+                const bool ok = row < from + rows;
+                auto at = [&](int s) { return attn_part(cut.first_run + s, s == 0) * a.part_rows + row; };
+                float l = 0.0f, mt = 0.0f;
+                float4 acc[2] = {make_float4(0, 0, 0, 0), make_float4(0, 0, 0, 0)};
+                if (ok) {
+                    // maximum and sum of up to 256 parts at a time, all their loads in flight
+                    float top = -INFINITY;
+                    for (int s0 = lane; s0 < parts; s0 += 256) {
+                        float2 r[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            r[k] = s0 + 32 * k < parts ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * at(s0 + 32 * k))
+                                                       : make_float2(-INFINITY, 0.0f);
+                        float t = top;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) t = fmaxf(t, r[k].x);
+                        const float t0 = t == -INFINITY ? 0.0f : t;
+                        l *= __builtin_amdgcn_exp2f(top - t0);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) l += r[k].y * __builtin_amdgcn_exp2f(r[k].x - t0);
+                        top = t;
+                    }
+                    float all = top;
+#pragma unroll
+                    for (int x = 16; x > 0; x /= 2) all = fmaxf(all, __shfl_xor(all, x, 32));
+                    mt = all == -INFINITY ? 0.0f : all;
+                    l *= __builtin_amdgcn_exp2f(top - mt);
+#pragma unroll
+                    for (int x = 16; x > 0; x /= 2) l += __shfl_xor(l, x, 32);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int d = k * 128 + lane * 4;
+                        if (d >= a.dim) continue;
+#pragma unroll 8
+                        for (int s = sub; s < parts; s += share) {
+                            const float wgt = __builtin_amdgcn_exp2f(a.part_ml[2 * at(s)] - mt);
+                            const float4 v = *reinterpret_cast<const float4 *>(a.part_o + at(s) * a.dim + d);
+                            acc[k].x = fmaf(wgt, v.x, acc[k].x);
+                            acc[k].y = fmaf(wgt, v.y, acc[k].y);
+                            acc[k].z = fmaf(wgt, v.z, acc[k].z);
+                            acc[k].w = fmaf(wgt, v.w, acc[k].w);
+                        }
+                    }
+                }
+                if (share > 1) {   // a workgroup's threads agree on it
+                    __syncthreads();
+                    sums[team][lane] = acc[0];
+                    sums[team][32 + lane] = acc[1];
+                    __syncthreads();
+                    if (sub == 0)
+                        for (int k = 1; k < share; ++k)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const float4 v = sums[team + k][32 * x + lane];
+                                acc[x].x += v.x;
+                                acc[x].y += v.y;
+                                acc[x].z += v.z;
+                                acc[x].w += v.w;
+                            }
+                }
+                if (!ok || sub) continue;
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                const int i = (int)div_by(cut.r0 + row, a.div_group);
+                const int head = cut.head * a.group + cut.r0 + row - i * a.group;
+                T *out = static_cast<T *>(a.o) + (long long)(cut.q0 + i) * a.os[0] + (long long)head * a.os[1];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int d = k * 128 + lane * 4;
+                    if (d < a.dim)
+                        store4(out + d, make_float4(acc[k].x * inv, acc[k].y * inv, acc[k].z * inv, acc[k].w * inv));
+                }
+                if (a.lse && lane == 0)
+                    a.lse[(long long)(cut.q0 + i) * a.kv_heads * a.group + head] =
+                        l == 0.0f ? -INFINITY : (mt + __log2f(l)) * 0.693147180559945309f;
+            }
+        }
+    }
 }
 
 }  // namespace
 
 hipError_t launch_attn_join(int dtype, const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
-    return dtype == FTCNN_F32 ? go<float>(pl, a, st) : go<uint16_t>(pl, a, st);
+    // rows of a unit to a workgroup, and workgroups to look through the runs: about 2048 in all
+    const int y = (pl.part_rows + pl.join_rows - 1) / pl.join_rows;
+    const dim3 grid((unsigned)std::min(pl.groups, std::max(64, 2048 / y)), (unsigned)y);
+    if (dtype == FTCNN_F32) attn_join_kernel<float><<<grid, kThreads, 0, st>>>(a, pl.join_rows);
+    else attn_join_kernel<uint16_t><<<grid, kThreads, 0, st>>>(a, pl.join_rows);
+    return hipGetLastError();
 }
 
 }  // namespace ftcnn

@@ -361,3 +361,26 @@ def test_nothing_to_do():
     one = torch.ones(1, dtype=torch.int32, device="cuda")
     out = paged.paged_attention(torch.ones(1, 4, 64, device="cuda"), kc, kc, none.view(1, 0), one)
     assert not out.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new,length,heads,window", [
+    ([1, 1], [70, 40], 2, 20), ([6], [50], 4, 0), ([60, 20], [130, 20], 2, 0), ([60], [300], 2, 25),
+    ([150], [150], 2, 0), ([150], [2100], 2, 40)])
+def test_what_a_row_does_not_see_may_be_infinite_or_nan(dtype, new, length, heads, window):
+    """Keys and values of later tokens, and of tokens that a window has left: the rows that do not see them
+    have what they have without them; those that do have an infinity or NaN."""
+    rng = np.random.default_rng([sum(length), heads, window])
+    q, kc, vc, lists, lens, starts = batch(rng, new, length, heads, 1, 64, dtype, 16)
+    for b, n in enumerate(length):
+        # an infinite value at the first key, one of either sign and a NaN at later ones, a NaN key
+        for j, (cache, at, x) in ((0, (vc, 3, float("inf"))), (n - 2, (vc, 5, float("-inf"))), (n // 2, (vc, 7, float("nan"))),
+                                  (n - 3, (vc, 11, float("inf"))),
+                                  (n - 1 if new[b] > 1 else 0, (kc, 1, float("nan")))):
+            if 0 <= j < n:
+                cache[lists[b, j // 16], j % 16, 0, at] = x
+    got = attend(q, kc, vc, lists, lens, starts, window=window, max_q=max(new), max_kv=max(length))
+    want = sv.attention(f64(q), f64(kc), f64(vc), lists, lens, starts, None, True, window, dtype)
+    near(got[0], want[0], np.nan_to_num(want[2], nan=0.0, posinf=0.0), "out")
+    near(got[1], want[1], np.nan_to_num(want[3], nan=0.0, posinf=0.0), "lse")
+    assert np.isfinite(want[0]).any()
