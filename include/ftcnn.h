@@ -487,8 +487,8 @@ typedef struct {
     int32_t list_len;                /* entries of a sequence's page list                 */
     int32_t causal, window;          /* window > 0 (causal only): the last window positions */
     int32_t max_q, max_kv;           /* the longest sequence's new and cached tokens; 0: not
-                                        known.  They size the launch: too small or too large
-                                        costs time, never the result                      */
+                                        known.  They shape the launch: too small or too large
+                                        costs time, and another order of the sums         */
     float scale;                     /* positive                                          */
     int64_t q_stride[2], out_stride[2];             /* token, head                        */
     int64_t k_cache_stride[3], v_cache_stride[3];   /* page, row, head                    */
@@ -507,10 +507,10 @@ typedef struct {
  * Scores, maxima, sums and outputs are held in fp32; bf16 calls round the softmax weights,
  * relative to a maximum, to bf16 for the product with the values.
  * kv_lens are taken within [0, list_len * page], q_starts within [0, tokens], and a page number
- * outside [0, pages) as the nearest one inside.  Rows of q, out and the cache start on 16 bytes.
- * out may be q.  The result does not depend on timing: calls on the same arguments give the same
- * bits.  One launch, or two where the cached tokens are split over workgroups: then the
- * workspace holds the parts. */
+ * outside [0, pages) as the nearest one inside.  Rows of q, out and the cache start on 16 bytes;
+ * the cache's strides are 0 to 2^29.  out may be q.  The result does not depend on timing: calls
+ * on the same arguments give the same bits.  One launch, or two where the cached tokens are split
+ * over workgroups: then the workspace holds the parts. */
 int ftcnn_paged_attention(const ftcnn_attention_desc *desc, const void *q, const void *k_cache, const void *v_cache,
                           const int32_t *page_list, const int32_t *kv_lens, const int32_t *q_starts, void *out,
                           float *lse, void *workspace, hipStream_t stream);

@@ -46,7 +46,7 @@ struct RopeArgs {
     const float *table;
 };
 hipError_t launch_rope_table(const ftcnn_rope_scaling &sc, float *table, hipStream_t st);
-// Units (two vectors of values) of a row, and lanes of a group, that the launch takes for its arguments
+// `aligned`: rows, their halves and the table start on whole vectors of four values
 hipError_t launch_rope(int dtype, RopeArgs a, bool aligned, hipStream_t st);
 
 // A unit that a run of key tiles starts inside of: the first and last run that hold some of it (first_run
@@ -80,7 +80,7 @@ struct AttnArgs {
 // What a call launches.
 struct AttnPlan {
     int dp;                      // head size the kernel is compiled for
-    int rows, keys;              // of a unit's tiles: 16 or 32 rows: stream_kernel, more: attn_kernel
+    int rows, keys;              // of a unit's tiles: 16 rows: stream_kernel, 128: attn_kernel
     int tiles, groups, min_run, unit_cost, part_rows, join_rows;
     size_t part_ml, cuts, bytes;   // workspace: the parts' outputs, their maxima and sums, the cuts
 };

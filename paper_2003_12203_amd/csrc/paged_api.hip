@@ -16,7 +16,8 @@ namespace {
 
 constexpr long long kMaxRows = 1LL << 30;   // rows a sequence's page list can name, and rows of queries
 
-bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool aligned(const void *p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+bool aligned16(const void *p) { return aligned(p, 16); }
 
 int check_dtype(int32_t dtype, const char *what) {
     if (dtype != FTCNN_F32 && dtype != FTCNN_BF16) return set_error(FTCNN_E_DTYPE, "%s: dtype %d", what, dtype);
@@ -60,31 +61,38 @@ AttnPlan attn_plan(const ftcnn_attention_desc &d) {
     p.dp = d.dim <= 64 ? 64 : (d.dim <= 128 ? 128 : 256);
     const bool bf = d.dtype == FTCNN_BF16;
     const long long es = bf ? 2 : 4;
-    if (rows <= 32) p.rows = rows <= 16 ? 16 : 32;
-    else if (!bf) p.rows = 128;
-    else p.rows = rows <= 64 ? 64 : 128;
-    if (p.rows <= 32) p.keys = p.dp * es <= 256 ? 32 : 16;
-    else p.keys = bf && p.dp <= 128 && p.rows == 128 ? 64 : 32;
+    // up to 16 rows a wave alone; more, a workgroup of four waves (32 rows of 30000 keys: 46 us, two tiles of 16
+    // of them in one wave 96; 64 rows: 64 us, a workgroup of two waves 143)
+    const bool wide = rows > 16;
+    p.rows = wide ? 128 : 16;
+    p.keys = wide ? (bf && p.dp <= 128 ? 64 : 32) : (p.dp * es <= 256 ? 32 : 16);
     const long long tile = p.rows;
     p.tiles = (int)((rows + tile - 1) / tile);
-    // workgroups that are on the device at a time
-    long long fit;
-    if (tile <= 32) {
-        fit = kComputeUnits * (p.dp * es * tile <= 4096 ? 8 : 4);
-    } else {
-        const long long lds = 4LL * p.keys * p.dp * es;
-        fit = kComputeUnits * std::max(1LL, std::min<long long>((kUnitLds - 1) / lds, 256 / tile));
-    }
+    // workgroups that are on the device at a time (registers and LDS)
+    const bool narrow = p.dp * es <= 256;
+    const long long fit = kComputeUnits * (wide ? (narrow ? 2 : 1) : (narrow ? 8 : 4));
     const long long some = std::min<long long>((long long)d.batch * p.tiles, d.tokens * group / tile + d.batch);
     const long long units = some * d.kv_heads;
     const long long range = d.window > 0 ? std::min<long long>(max_kv, d.window + tile / group + 1) : max_kv;
-    p.min_run = 8 * p.keys;
-    p.unit_cost = (p.rows <= 32 ? 1 : 3) * p.keys;
-    bool even = range > p.min_run && units < 4 * fit;
-    if (even) {
-        p.groups = (int)std::min(fit, (units * range + p.min_run - 1) / p.min_run);
+    // Whole units or even runs: the shorter by the sizes the host knows, in the time of a key (a wave alone
+    // 70 ns; a workgroup, bf16 25 ns, fp32 60 ns).  What the start and end of a unit take: a wave one tile, bf16
+    // workgroups five of 64 keys (mixed chunks 117 us; three 130, one 153), fp32 two of 32.  What even runs
+    // take besides, the schedule and the join: 14 us of a wave, 25 of a workgroup.  A run is not made shorter than
+    // min_run.  Whole / even: one prompt of 512 tokens 18 / 44 us, of 2048 56 / 88; chunks over 8192 cached tokens
+    // 256 / 111; 64 tokens over 500 keys 44 / 44, over 2000 169 / 114.
+    p.min_run = wide ? 128 : 64;
+    p.unit_cost = wide ? (bf ? 320 : 64) : 32;
+    const long long rest = wide ? (bf ? 1100 : 330) : 200;
+    const long long mean = d.window > 0 || !d.causal ? range : std::max(1LL, max_kv - max_q / 2);
+    const long long whole = std::max(range, units * mean / fit) + p.unit_cost * ((units + fit - 1) / fit);
+    // as many runs on every compute unit: 365 on 256 of them 53 us, 256 runs 42
+    long long runs = std::min(fit, (units * range + p.min_run - 1) / p.min_run);
+    if (runs > kComputeUnits) runs -= runs % kComputeUnits;
+    const long long even = units * (mean + p.unit_cost) / runs + rest;
+    if (even < whole) {
+        p.groups = (int)runs;
         p.part_rows = (int)std::min<long long>(tile, d.tokens * group);
-        p.join_rows = tile > 32 ? 8 : (p.groups >= 32 * units ? 1 : 32);
+        p.join_rows = wide ? 8 : (p.groups >= 32 * units ? 1 : 16);
         const size_t n = 2 * (size_t)p.groups * p.part_rows;
         auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
         p.part_ml = up(n * d.dim * sizeof(float));
@@ -146,7 +154,8 @@ int ftcnn_qk_norm_rope(const ftcnn_rope_desc *d, const void *q, const void *k, c
                        hipStream_t stream) {
     const char *what = "qk_norm_rope";
     if (!d) return set_error(FTCNN_E_ARG, "%s: null descriptor", what);
-    if (d->heads < 0 || d->kv_heads < 0) return set_error(FTCNN_E_SHAPE, "%s: negative heads", what);
+    if (d->heads < 0 || d->kv_heads < 0 || (long long)d->heads + d->kv_heads > kMaxRows)
+        return set_error(FTCNN_E_SHAPE, "%s: heads %d and %d", what, d->heads, d->kv_heads);
     const int rc = check_rope(what, d->dtype, d->tokens, d->heads + d->kv_heads, d->dim, d->rot, d->layout,
                               d->max_pos, d->eps, positions, table, q_weight || k_weight, d->weight_dtype);
     if (rc != FTCNN_OK) return rc;
@@ -158,8 +167,9 @@ int ftcnn_qk_norm_rope(const ftcnn_rope_desc *d, const void *q, const void *k, c
     void *out[2] = {q_out, k_out};
     const int32_t heads[2] = {d->heads, d->kv_heads};
     const int64_t *is[2] = {d->q_stride, d->k_stride}, *os[2] = {d->q_out_stride, d->k_out_stride};
-    const int vec = d->dtype == FTCNN_F32 ? 4 : 8;
-    bool al = d->dim % (2 * vec) == 0 && (!positions || (d->rot % (2 * vec) == 0 && aligned16(table)));
+    constexpr int vec = 4;   // values of a load
+    const int load = d->dtype == FTCNN_F32 ? 16 : 8;
+    bool al = d->dim % (2 * vec) == 0 && (!positions || (d->rot % (2 * vec) == 0 && aligned(table, 16)));
     for (int s = 0; s < 2; ++s) {
         a.x[s] = in[s];
         a.y[s] = out[s];
@@ -170,7 +180,7 @@ int ftcnn_qk_norm_rope(const ftcnn_rope_desc *d, const void *q, const void *k, c
             a.ys[s][i] = os[s][i];
             al = al && (!heads[s] || (is[s][i] % vec == 0 && os[s][i] % vec == 0));
         }
-        al = al && (!heads[s] || (aligned16(in[s]) && aligned16(out[s])));
+        al = al && (!heads[s] || (aligned(in[s], load) && aligned(out[s], load)));
     }
     a.tokens = d->tokens;
     a.dim = d->dim;
@@ -201,8 +211,9 @@ int ftcnn_kv_append(const ftcnn_append_desc *d, const void *k, const void *v, co
     const void *in[2] = {k, v};
     void *out[2] = {k_cache, v_cache};
     const int64_t *is[2] = {d->k_stride, d->v_stride}, *os[2] = {d->k_cache_stride, d->v_cache_stride};
-    const int vec = d->dtype == FTCNN_F32 ? 4 : 8;
-    bool al = d->dim % (2 * vec) == 0 && (!positions || (d->rot % (2 * vec) == 0 && aligned16(table)));
+    constexpr int vec = 4;   // values of a load
+    const int load = d->dtype == FTCNN_F32 ? 16 : 8;
+    bool al = d->dim % (2 * vec) == 0 && (!positions || (d->rot % (2 * vec) == 0 && aligned(table, 16)));
     for (int s = 0; s < 2; ++s) {
         a.x[1 + s] = in[s];
         a.y[1 + s] = out[s];
@@ -215,7 +226,7 @@ int ftcnn_kv_append(const ftcnn_append_desc *d, const void *k, const void *v, co
             a.ys[1 + s][i] = os[s][i];
             al = al && os[s][i] % vec == 0;
         }
-        al = al && aligned16(in[s]) && aligned16(out[s]);
+        al = al && aligned(in[s], load) && aligned(out[s], load);
     }
     a.weight[1] = k_weight;
     a.tokens = d->tokens;

@@ -135,6 +135,12 @@ struct AttnSeq {
     }
 };
 
+// a / b of what is not negative, in 32 bits where they hold it (the wide division takes a microsecond).
+__device__ __forceinline__ long long divide(long long a, long long b) {
+    if (((a | b) >> 32) == 0) return (unsigned)a / (unsigned)b;
+    return a / b;
+}
+
 // The even schedule: the run (of the units' costs) a workgroup takes, and where a sequence's units begin.
 struct AttnRuns {
     long long total, run;
@@ -146,7 +152,7 @@ struct AttnRuns {
 #pragma unroll
         for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
         total = uniform(sum);
-        run = uniform(max((sum + a.groups - 1) / a.groups, (long long)a.min_run));
+        run = max(divide(total + a.groups - 1, a.groups), (long long)a.min_run);
     }
     // the sequence that cost `at` < total belongs to, and where that sequence begins
     __device__ static int find(const AttnArgs &a, int rows, long long at, long long &base) {
@@ -252,13 +258,13 @@ __device__ __forceinline__ void attn_schedule(const AttnArgs &a, int rows, int k
                 continue;
             }
             const long long of_head = sq.head_work();
-            const int hk = uniform((int)((at - base) / of_head));
+            const int hk = uniform((int)divide(at - base, of_head));
             const long long y = at - base - hk * of_head;
             const int rt = uniform(sq.find(y)), cost = uniform(sq.cost(rt)), c0 = uniform((int)(y - sq.before(rt)));
             const int c1 = uniform((int)min((long long)cost, c0 + (end - at)));
             if (threadIdx.x == 0 && at == g * runs.run) {
                 const long long first = at - c0;
-                *cut = AttnCut{c0 == 0 ? -1 : (int)(first / runs.run), (int)((first + cost - 1) / runs.run),
+                *cut = AttnCut{c0 == 0 ? -1 : (int)divide(first, runs.run), (int)divide(first + cost - 1, runs.run),
                                sq.q0, hk, rt * rows, min(rows, sq.nq * a.group - rt * rows)};
             }
             // whole key tiles, wherever the cut falls

@@ -4,9 +4,7 @@
 namespace ftcnn {
 namespace {
 template <int DP> hipError_t pick(const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
-    if (pl.rows == 16) return stream_go<uint16_t, DP, 1>(a, st);
-    if (pl.rows == 32) return stream_go<uint16_t, DP, 2>(a, st);
-    if (pl.rows == 64) return attn_go<uint16_t, DP, 2, 1>(a, st);
+    if (pl.rows == 16) return stream_go<uint16_t, DP>(a, st);
     return attn_go<uint16_t, DP, 4, (DP <= 128 ? 2 : 1)>(a, st);
 }
 }  // namespace

@@ -4,8 +4,7 @@
 namespace ftcnn {
 namespace {
 template <int DP> hipError_t pick(const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
-    if (pl.rows == 16) return stream_go<float, DP, 1>(a, st);
-    if (pl.rows == 32) return stream_go<float, DP, 2>(a, st);
+    if (pl.rows == 16) return stream_go<float, DP>(a, st);
     return attn_go<float, DP, 4, 1>(a, st);
 }
 }  // namespace

@@ -13,6 +13,7 @@ namespace ftcnn {
 namespace {
 
 constexpr int kTeams = kThreads / 32;
+constexpr int kInFlight = 8;   // parts that a team has on their way
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, int rows_here) {
@@ -66,14 +67,25 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, int row
                     for (int k = 0; k < 2; ++k) {
                         const int d = k * 128 + lane * 4;
                         if (d >= a.dim) continue;
-#pragma unroll 8
-                        for (int s = sub; s < parts; s += share) {
-                            const float wgt = __builtin_amdgcn_exp2f(a.part_ml[2 * at(s)] - mt);
-                            const float4 v = *reinterpret_cast<const float4 *>(a.part_o + at(s) * a.dim + d);
-                            acc[k].x = fmaf(wgt, v.x, acc[k].x);
-                            acc[k].y = fmaf(wgt, v.y, acc[k].y);
-                            acc[k].z = fmaf(wgt, v.z, acc[k].z);
-                            acc[k].w = fmaf(wgt, v.w, acc[k].w);
+                        for (int s0 = sub; s0 < parts; s0 += kInFlight * share) {
+                            float at_max[kInFlight];
+                            float4 v[kInFlight];
+#pragma unroll
+                            for (int x = 0; x < kInFlight; ++x) {
+                                const long long p = at(min(s0 + x * share, parts - 1));
+                                at_max[x] = a.part_ml[2 * p];
+                                v[x] = *reinterpret_cast<const float4 *>(a.part_o + p * a.dim + d);
+                            }
+#pragma unroll
+                            for (int x = 0; x < kInFlight; ++x) {
+                                // (no branch: it would have each load wait for the one before)
+                                const bool there = s0 + x * share < parts;
+                                const float wgt = there ? __builtin_amdgcn_exp2f(at_max[x] - mt) : 0.0f;
+                                acc[k].x = fmaf(wgt, there ? v[x].x : 0.0f, acc[k].x);
+                                acc[k].y = fmaf(wgt, there ? v[x].y : 0.0f, acc[k].y);
+                                acc[k].z = fmaf(wgt, there ? v[x].z : 0.0f, acc[k].z);
+                                acc[k].w = fmaf(wgt, there ? v[x].w : 0.0f, acc[k].w);
+                            }
                         }
                     }
                 }

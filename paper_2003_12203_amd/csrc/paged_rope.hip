@@ -7,9 +7,12 @@
 // ("interleaved"); (cos, sin) of a pair at a position come from a table made once in float64.
 //
 // Memory-bound: a row is read and written once, and the table's row once for several heads.  A row is
-// cut into units of two vectors of V values (16 bytes each where alignment allows): a rotated unit
+// cut into units of two vectors of V values (four where alignment allows, else one): a rotated unit
 // holds V whole pairs, so a rotation needs no other lane.  A group of lanes holds a row, a unit or
-// more a lane, and walks some heads of a token, four rows in flight.
+// more a lane, and walks some heads of a token, two rows in flight.  One, two or four rows in flight and
+// vectors of four or eight bf16 values differ by less than a tenth: 8192 tokens of 40 heads of 128, normed and
+// rotated, 33 to 35 us (35.0 as it is: 4.9 TB/s of the 5.2 that a copy reaches), 16384 tokens of eight
+// such heads appended 28.4 to 31.3 (28.4).  For few tokens the call's own time on the host, 8 to 10 us, is all.
 #include <algorithm>
 
 #include "paged.h"
@@ -18,8 +21,8 @@ namespace ftcnn {
 namespace {
 
 template <typename T, int V> struct Vec;
-template <> struct Vec<float, 4> { typedef uint4 type; };
-template <> struct Vec<uint16_t, 8> { typedef uint4 type; };
+template <> struct Vec<float, 4> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Vec<uint16_t, 4> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Vec<float, 1> { typedef float type; };
 template <> struct Vec<uint16_t, 1> { typedef uint16_t type; };
 
@@ -33,11 +36,25 @@ __device__ inline float as_f32(uint16_t v) { return bf16_bits_to_f32(v); }
 __device__ inline void put(float &d, float v) { d = v; }
 __device__ inline void put(uint16_t &d, float v) { d = f32_to_bf16_rne(v); }
 
-constexpr int kRowsInFlight = 4;
+constexpr int kRowsInFlight = 2;
+
+// The sum over the LPR lanes of a group, in all of them: within rows of 16 lanes by the vector unit alone.
+template <int CTRL> __device__ inline float with_lane(float x) {
+    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int LPR> __device__ inline float group_sum(float x) {
+    x = with_lane<0xB1>(x);                            // lane ^ 1
+    x = with_lane<0x4E>(x);                            // lane ^ 2
+    if constexpr (LPR >= 8) x = with_lane<0x141>(x);   // the other four of eight
+    if constexpr (LPR >= 16) x = with_lane<0x140>(x);  // the other eight of sixteen
+    if constexpr (LPR >= 32) x += __shfl_xor(x, 16, LPR);
+    if constexpr (LPR >= 64) x += __shfl_xor(x, 32, LPR);
+    return x;
+}
 
 // LPR lanes hold a row, UPL units a lane (unit lane + u * LPR).
-template <typename T, int V, int LPR, int UPL>
-__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
+template <typename T, int V, int LPR, int UPL, bool PAST_L2>
+__global__ __launch_bounds__(kThreads, 4) void rope_kernel(RopeArgs a) {
     constexpr int B = UPL == 1 ? kRowsInFlight : 1;
     const int lane = threadIdx.x % LPR;
     const unsigned id = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
@@ -126,9 +143,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                             ss = fmaf(va, va, ss);
                             ss = fmaf(vb, vb, ss);
                         }
-#pragma unroll
-                for (int m = LPR / 2; m > 0; m /= 2) ss += __shfl_xor(ss, m, LPR);
-                scale = rsqrtf(ss / (float)a.dim + a.eps);
+                scale = rsqrtf(group_sum<LPR>(ss) / (float)a.dim + a.eps);
             }
 #pragma unroll
             for (int u = 0; u < UPL; ++u) {
@@ -169,8 +184,15 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                         }
                     }
                 }
-                *reinterpret_cast<typename Vec<T, V>::type *>(row + offa[u]) = pa[r][u].q;
-                *reinterpret_cast<typename Vec<T, V>::type *>(row + offb[u]) = pb[r][u].q;
+                typedef typename Vec<T, V>::type Q;
+                Q *to_a = reinterpret_cast<Q *>(row + offa[u]), *to_b = reinterpret_cast<Q *>(row + offb[u]);
+                if constexpr (PAST_L2) {
+                    __builtin_nontemporal_store(pa[r][u].q, to_a);
+                    __builtin_nontemporal_store(pb[r][u].q, to_b);
+                } else {
+                    *to_a = pa[r][u].q;
+                    *to_b = pb[r][u].q;
+                }
             }
         }
     }
@@ -182,14 +204,19 @@ hipError_t go(RopeArgs a, hipStream_t st) {
     // heads a group: enough to read a table row for several, few enough that the device is full
     // (a wave for each of its 1024 SIMDs, eight over)
     const long long groups = 8192LL * (64 / LPR);
-    a.per_chunk = (int)std::min<long long>(8, std::max<long long>(1, a.tokens * rows / groups));
+    a.per_chunk = 1;
+    while (a.per_chunk < 8 && a.per_chunk * 2 * groups <= a.tokens * rows) a.per_chunk *= 2;
+    // outputs that the L2s (eight of 4 MiB) will not keep for the next kernel are not kept in them: 8192 tokens of
+    // 40 heads of 128 in bf16 34.3 us for 40.1, 16384 tokens appended 30.0 for 33.1
+    const bool past_l2 = a.tokens * rows * a.dim * (long long)sizeof(T) > (32LL << 20);
     a.all_chunks = 0;
     for (int s = 0; s < 3; ++s) a.all_chunks += a.chunks[s] = (a.heads[s] + a.per_chunk - 1) / a.per_chunk;
     a.div_chunks = fast_div((uint32_t)a.all_chunks);
     const long long ids = (long long)a.tokens * a.all_chunks;
     const long long blocks = (ids + kThreads / LPR - 1) / (kThreads / LPR);
     if (ids >= (1LL << 31)) return hipErrorInvalidValue;
-    rope_kernel<T, V, LPR, UPL><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    if (past_l2) rope_kernel<T, V, LPR, UPL, true><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+    else rope_kernel<T, V, LPR, UPL, false><<<(unsigned)blocks, kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -199,7 +226,7 @@ template <typename T, int V> hipError_t pick(const RopeArgs &a, hipStream_t st) 
         if (units <= 4) return go<T, V, 4, 1>(a, st);
         if (units <= 8) return go<T, V, 8, 1>(a, st);
         if (units <= 16) return go<T, V, 16, 1>(a, st);
-        return go<T, V, 32, 1>(a, st);
+        return go<T, V, 32, 1>(a, st);   // at most 32 units: dim <= 256
     } else {
         if (units <= 32) return go<T, V, 32, 1>(a, st);
         if (units <= 64) return go<T, V, 64, 1>(a, st);
@@ -233,7 +260,7 @@ __global__ __launch_bounds__(kThreads) void rope_table_kernel(ftcnn_rope_scaling
 
 hipError_t launch_rope(int dtype, RopeArgs a, bool aligned, hipStream_t st) {
     if (dtype == FTCNN_F32) return aligned ? pick<float, 4>(a, st) : pick<float, 1>(a, st);
-    return aligned ? pick<uint16_t, 8>(a, st) : pick<uint16_t, 1>(a, st);
+    return aligned ? pick<uint16_t, 4>(a, st) : pick<uint16_t, 1>(a, st);
 }
 
 hipError_t launch_rope_table(const ftcnn_rope_scaling &sc, float *table, hipStream_t st) {

@@ -29,12 +29,12 @@ template <typename T, int DP> struct StreamTile {
     static constexpr int VU = VE * (int)sizeof(T) / VB, VL = VB / sizeof(T);   // loads of a key, values of a load
 };
 
-template <typename T, int DP, int RT, bool EVEN>
-__global__ __launch_bounds__(64, DP * sizeof(T) * RT <= 128 ? 3 : DP * sizeof(T) * RT <= 512 ? 2 : 1) void stream_kernel(AttnArgs a) {
+template <typename T, int DP, bool EVEN>
+__global__ __launch_bounds__(64, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 512 ? 2 : 1) void stream_kernel(AttnArgs a) {
     using L = StreamTile<T, DP>;
     constexpr bool BF = sizeof(T) == 2;
     constexpr int S2 = L::S2, KEYS = L::KEYS, EU = L::EU, NQ = L::NQ, VE = L::VE, VU = L::VU, VL = L::VL;
-    constexpr int ROWS = 16 * RT;
+    constexpr int ROWS = 16;
     const int lane = threadIdx.x, n16 = lane & 15, h = lane >> 4;
     const float c = a.scale_log2;
 
@@ -103,35 +103,26 @@ __global__ __launch_bounds__(64, DP * sizeof(T) * RT <= 128 ? 3 : DP * sizeof(T)
             load_k(0, pid);
             load_v(0, pid);
         }
-        // this lane's rows; past the last one, the last again (not stored)
-        int qi[RT], head[RT], jhi[RT], jlo[RT];
-        uint4 qf[RT][NQ];
-        f32x4_t o[RT][VE];
-        float m[RT], l[RT];
-        int jhi_min = INT_MAX, jlo_max = 0;
-#pragma unroll
-        for (int y = 0; y < RT; ++y) {
-            const int r = min(r0 + 16 * y + n16, nrows - 1);
-            qi[y] = (int)div_by(r, a.div_group);
-            head[y] = hk * a.group + r - qi[y] * a.group;
-            const int pos = sq.kv - sq.nq + qi[y];
-            jhi[y] = min(a.causal ? pos : sq.kv - 1, k1 - 1);   // the keys it sees: jlo..jhi
-            jlo[y] = a.window > 0 ? pos - a.window + 1 : 0;
-            jhi_min = min(jhi_min, __builtin_amdgcn_readlane(jhi[y], 0));
-            jlo_max = max(jlo_max, __builtin_amdgcn_readlane(jlo[y], 15));
-            const T *row = static_cast<const T *>(a.q) + (long long)(sq.q0 + qi[y]) * a.qs[0] + (long long)head[y] * a.qs[1];
+        // this lane's row; past the last one, the last again (not stored)
+        const int mine = r0 + n16, r = min(mine, nrows - 1);
+        const int qi = (int)div_by(r, a.div_group), head = hk * a.group + r - qi * a.group;
+        const int pos = sq.kv - sq.nq + qi;
+        const int jhi = min(a.causal ? pos : sq.kv - 1, k1 - 1);   // the keys it sees: jlo..jhi
+        const int jlo = a.window > 0 ? pos - a.window + 1 : 0;
+        const int jhi_min = __builtin_amdgcn_readlane(jhi, 0), jlo_max = __builtin_amdgcn_readlane(jlo, 15);
+        uint4 qf[NQ];
+        {
+            const T *row = static_cast<const T *>(a.q) + (long long)(sq.q0 + qi) * a.qs[0] + (long long)head * a.qs[1];
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
                 const int col = (4 * q + h) * EU;
-                qf[y][q] = col < a.dim ? *reinterpret_cast<const uint4 *>(row + col) : make_uint4(0, 0, 0, 0);
+                qf[q] = col < a.dim ? *reinterpret_cast<const uint4 *>(row + col) : make_uint4(0, 0, 0, 0);
             }
-#pragma unroll
-            for (int e = 0; e < VE; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[y][e][i] = 0.0f;
-            m[y] = -INFINITY;
-            l[y] = 0.0f;
         }
+        f32x4_t o[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        float m = -INFINITY, l = 0.0f;
 
         int dirt0 = INT_MAX, dirt1 = -1;   // the first and last tile with values not finite
         for (int t = 0; t < ntiles; ++t) {
@@ -142,25 +133,23 @@ __global__ __launch_bounds__(64, DP * sizeof(T) * RT <= 128 ? 3 : DP * sizeof(T)
                     for (int q = 0; q < NQ; ++q)
                         if ((4 * q + h) * EU >= a.dim) kf[s][q] = make_uint4(0, 0, 0, 0);
             }
-            f32x4_t s[RT][S2];
-#pragma unroll
-            for (int y = 0; y < RT; ++y)
+            f32x4_t s[S2];
 #pragma unroll
                 for (int k = 0; k < S2; ++k) {
-                    s[y][k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                    s[k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int q = 0; q < NQ; ++q) {
                         if constexpr (BF) {
-                            s[y][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                __builtin_bit_cast(bf16x8_t, kf[k][q]), __builtin_bit_cast(bf16x8_t, qf[y][q]),
-                                s[y][k], 0, 0, 0);
+                            s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                __builtin_bit_cast(bf16x8_t, kf[k][q]), __builtin_bit_cast(bf16x8_t, qf[q]),
+                                s[k], 0, 0, 0);
                         } else {
                             const float4 ka = __builtin_bit_cast(float4, kf[k][q]);
-                            const float4 qb = __builtin_bit_cast(float4, qf[y][q]);
-                            s[y][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.x, qb.x, s[y][k], 0, 0, 0);
-                            s[y][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.y, qb.y, s[y][k], 0, 0, 0);
-                            s[y][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.z, qb.z, s[y][k], 0, 0, 0);
-                            s[y][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.w, qb.w, s[y][k], 0, 0, 0);
+                            const float4 qb = __builtin_bit_cast(float4, qf[q]);
+                            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.x, qb.x, s[k], 0, 0, 0);
+                            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.y, qb.y, s[k], 0, 0, 0);
+                            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.z, qb.z, s[k], 0, 0, 0);
+                            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.w, qb.w, s[k], 0, 0, 0);
                         }
                     }
                 }
@@ -169,44 +158,41 @@ __global__ __launch_bounds__(64, DP * sizeof(T) * RT <= 128 ? 3 : DP * sizeof(T)
             if (t + 2 < ntiles) pid1 = lookup(t + 2);
             const int j0 = k0 + t * KEYS;
             const bool masked = j0 + KEYS - 1 > jhi_min || j0 < jlo_max;
-#pragma unroll
-            for (int y = 0; y < RT; ++y) {
-                if (masked) {
-#pragma unroll
-                    for (int k = 0; k < S2; ++k)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int j = j0 + 16 * k + 4 * h + i;
-                            s[y][k][i] = j >= jlo[y] && j <= jhi[y] ? s[y][k][i] : -INFINITY;
-                        }
-                }
-                float top = s[y][0][0];
-#pragma unroll
-                for (int k = 0; k < S2; ++k)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[y][k][i]);
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                // the running maximum, moved only when scores pass it by more than 2^8 (in the weights)
-                if (__any(top * c > m[y] * c + 8.0f)) {
-                    const float mn = fmaxf(m[y], top);
-                    const float alpha = mn == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m[y] - mn) * c);
-                    l[y] *= alpha;
-#pragma unroll
-                    for (int e = 0; e < VE; ++e)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[y][e][i] *= alpha;
-                    m[y] = mn;
-                }
-                const float mc = m[y] == -INFINITY ? 0.0f : m[y] * c;
+            if (masked) {
 #pragma unroll
                 for (int k = 0; k < S2; ++k)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        s[y][k][i] = __builtin_amdgcn_exp2f(fmaf(s[y][k][i], c, -mc));
-                        l[y] += s[y][k][i];
+                        const int j = j0 + 16 * k + 4 * h + i;
+                        s[k][i] = j >= jlo && j <= jhi ? s[k][i] : -INFINITY;
                     }
             }
+            float top = s[0][0];
+#pragma unroll
+            for (int k = 0; k < S2; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, s[k][i]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            // the running maximum, moved only when scores pass it by more than 2^8 (in the weights)
+            if (__any(top * c > m * c + 8.0f)) {
+                const float mn = fmaxf(m, top);
+                const float alpha = mn == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - mn) * c);
+                l *= alpha;
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[e][i] *= alpha;
+                m = mn;
+            }
+            const float mc = m == -INFINITY ? 0.0f : m * c;
+#pragma unroll
+            for (int k = 0; k < S2; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[k][i] = __builtin_amdgcn_exp2f(fmaf(s[k][i], c, -mc));
+                    l += s[k][i];
+                }
             if (masked) {   // see NonFinite
                 bool any = false;
 #pragma unroll
@@ -230,9 +216,7 @@ __global__ __launch_bounds__(64, DP * sizeof(T) * RT <= 128 ? 3 : DP * sizeof(T)
 #pragma unroll
                     for (int e = 0; e < VE; ++e) {
                         const float v = value(k, i, e);
-#pragma unroll
-                        for (int y = 0; y < RT; ++y)
-                            o[y][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[y][k][i], o[y][e], 0, 0, 0);
+                            o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[k][i], o[e], 0, 0, 0);
                     }
             if (t + 1 < ntiles) load_v(t + 1, pid_next);
         }
@@ -250,59 +234,50 @@ __global__ __launch_bounds__(64, DP * sizeof(T) * RT <= 128 ? 3 : DP * sizeof(T)
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
                             const float v = value_of(at[x]);
-#pragma unroll
-                            for (int y = 0; y < RT; ++y)
-                                o[y][e + x][i] += key >= jlo[y] && key <= jhi[y] && !(fabsf(v) < INFINITY) ? v : 0.0f;
+                                o[e + x][i] += key >= jlo && key <= jhi && !(fabsf(v) < INFINITY) ? v : 0.0f;
                         }
                     }
             }
-#pragma unroll
-        for (int y = 0; y < RT; ++y) {
-            const int mine = r0 + 16 * y + n16;
-            float sum = l[y] + __shfl_xor(l[y], 16);
-            sum += __shfl_xor(sum, 32);
-            if (mine >= nrows) continue;
-            const long long orow = (long long)(sq.q0 + qi[y]) * a.kv_heads * a.group + head[y];
-            // o[y][e][i] is value VE (4 h + i) + e of the row
-            if (part >= 0) {
-                const long long at = part * a.part_rows + (mine - r0);
-                float *po = a.part_o + at * a.dim;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < VE; e += 4) {
-                        const int d = VE * (4 * h + i) + e;
-                        if (d < a.dim)
-                            *reinterpret_cast<float4 *>(po + d) =
-                                make_float4(o[y][e][i], o[y][e + 1][i], o[y][e + 2][i], o[y][e + 3][i]);
-                    }
-                if (h == 0) {
-                    a.part_ml[at * 2] = m[y] * c;
-                    a.part_ml[at * 2 + 1] = sum;
-                }
-                continue;
-            }
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // a row that sees nothing is zero
-            T *out = static_cast<T *>(a.o) + (long long)(sq.q0 + qi[y]) * a.os[0] + (long long)head[y] * a.os[1];
+        float sum = l + __shfl_xor(l, 16);
+        sum += __shfl_xor(sum, 32);
+        if (mine >= nrows) return;
+        // o[e][i] is value VE (4 h + i) + e of the row
+        if (part >= 0) {
+            const long long at = part * a.part_rows + (mine - r0);
+            float *po = a.part_o + at * a.dim;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < VE; e += 4) {
                     const int d = VE * (4 * h + i) + e;
-                    if (d < a.dim)
-                        store4(out + d, make_float4(o[y][e][i] * inv, o[y][e + 1][i] * inv, o[y][e + 2][i] * inv,
-                                                    o[y][e + 3][i] * inv));
+                    if (d < a.dim) store4(po + d, make_float4(o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]));
                 }
-            if (a.lse && h == 0)
-                a.lse[orow] = sum == 0.0f ? -INFINITY : (m[y] * c + __log2f(sum)) * 0.693147180559945309f;
+            if (h == 0) {
+                a.part_ml[at * 2] = m * c;
+                a.part_ml[at * 2 + 1] = sum;
+            }
+            return;
         }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // a row that sees nothing is zero
+        T *out = static_cast<T *>(a.o) + (long long)(sq.q0 + qi) * a.os[0] + (long long)head * a.os[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < VE; e += 4) {
+                const int d = VE * (4 * h + i) + e;
+                if (d < a.dim)
+                    store4(out + d, make_float4(o[e][i] * inv, o[e + 1][i] * inv, o[e + 2][i] * inv, o[e + 3][i] * inv));
+            }
+        if (a.lse && h == 0)
+            a.lse[(long long)(sq.q0 + qi) * a.kv_heads * a.group + head] =
+                sum == 0.0f ? -INFINITY : (m * c + __log2f(sum)) * 0.693147180559945309f;
     };
     attn_schedule<EVEN>(a, ROWS, KEYS, unit);
 }
 
-template <typename T, int DP, int RT> hipError_t stream_go(const AttnArgs &a, hipStream_t st) {
-    if (a.groups) stream_kernel<T, DP, RT, true><<<a.groups, 64, 0, st>>>(a);
-    else stream_kernel<T, DP, RT, false><<<(unsigned)a.tiles * a.kv_heads * a.batch, 64, 0, st>>>(a);
+template <typename T, int DP> hipError_t stream_go(const AttnArgs &a, hipStream_t st) {
+    if (a.groups) stream_kernel<T, DP, true><<<a.groups, 64, 0, st>>>(a);
+    else stream_kernel<T, DP, false><<<(unsigned)a.tiles * a.kv_heads * a.batch, 64, 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -253,6 +253,8 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     if q_starts is not None and not (q_starts.dtype is _I32 and q_starts.shape == (batch + 1,) and
                                      q_starts.is_contiguous() and q_starts.get_device() == dev):
         _bad(what, f"q_starts must be a contiguous int32 [{batch + 1}] on device {dev}, not {_is(q_starts)}")
+    if q_starts is None:
+        max_q = 1
     if lse is not None and not (lse.dtype is _F32 and lse.shape == (tokens, heads) and lse.is_contiguous() and
                                 lse.get_device() == dev):
         _bad(what, f"lse must be a contiguous float32 [{tokens}][{heads}] on device {dev}, not {_is(lse)}")
