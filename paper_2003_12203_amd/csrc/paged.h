@@ -46,8 +46,7 @@ struct RopeArgs {
     const float *table;
 };
 hipError_t launch_rope_table(const ftcnn_rope_scaling &sc, float *table, hipStream_t st);
-// `aligned`: rows, their halves and the table start on whole vectors of four values
-hipError_t launch_rope(int dtype, RopeArgs a, bool aligned, hipStream_t st);
+hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st);
 
 // A unit that a run of key tiles starts inside of: the first and last run that hold some of it (first_run
 // < 0: the run starts with a unit, or is empty), the first row of its sequence's queries, its key head,

@@ -16,8 +16,7 @@ namespace {
 
 constexpr long long kMaxRows = 1LL << 30;   // rows a sequence's page list can name, and rows of queries
 
-bool aligned(const void *p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-bool aligned16(const void *p) { return aligned(p, 16); }
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 int check_dtype(int32_t dtype, const char *what) {
     if (dtype != FTCNN_F32 && dtype != FTCNN_BF16) return set_error(FTCNN_E_DTYPE, "%s: dtype %d", what, dtype);
@@ -167,9 +166,6 @@ int ftcnn_qk_norm_rope(const ftcnn_rope_desc *d, const void *q, const void *k, c
     void *out[2] = {q_out, k_out};
     const int32_t heads[2] = {d->heads, d->kv_heads};
     const int64_t *is[2] = {d->q_stride, d->k_stride}, *os[2] = {d->q_out_stride, d->k_out_stride};
-    constexpr int vec = 4;   // values of a load
-    const int load = d->dtype == FTCNN_F32 ? 16 : 8;
-    bool al = d->dim % (2 * vec) == 0 && (!positions || (d->rot % (2 * vec) == 0 && aligned(table, 16)));
     for (int s = 0; s < 2; ++s) {
         a.x[s] = in[s];
         a.y[s] = out[s];
@@ -178,9 +174,7 @@ int ftcnn_qk_norm_rope(const ftcnn_rope_desc *d, const void *q, const void *k, c
         for (int i = 0; i < 2; ++i) {
             a.xs[s][i] = is[s][i];
             a.ys[s][i] = os[s][i];
-            al = al && (!heads[s] || (is[s][i] % vec == 0 && os[s][i] % vec == 0));
         }
-        al = al && (!heads[s] || (aligned(in[s], load) && aligned(out[s], load)));
     }
     a.tokens = d->tokens;
     a.dim = d->dim;
@@ -191,7 +185,7 @@ int ftcnn_qk_norm_rope(const ftcnn_rope_desc *d, const void *q, const void *k, c
     a.eps = d->eps;
     a.positions = positions;
     a.table = table;
-    FT_PAGED_HIP(launch_rope(d->dtype, a, al, stream), what);
+    FT_PAGED_HIP(launch_rope(d->dtype, a, stream), what);
     return FTCNN_OK;
 }
 
@@ -211,22 +205,14 @@ int ftcnn_kv_append(const ftcnn_append_desc *d, const void *k, const void *v, co
     const void *in[2] = {k, v};
     void *out[2] = {k_cache, v_cache};
     const int64_t *is[2] = {d->k_stride, d->v_stride}, *os[2] = {d->k_cache_stride, d->v_cache_stride};
-    constexpr int vec = 4;   // values of a load
-    const int load = d->dtype == FTCNN_F32 ? 16 : 8;
-    bool al = d->dim % (2 * vec) == 0 && (!positions || (d->rot % (2 * vec) == 0 && aligned(table, 16)));
     for (int s = 0; s < 2; ++s) {
         a.x[1 + s] = in[s];
         a.y[1 + s] = out[s];
         a.heads[1 + s] = d->kv_heads;
         for (int i = 0; i < 3; ++i) {
-            if (i < 2) {
-                a.xs[1 + s][i] = is[s][i];
-                al = al && is[s][i] % vec == 0;
-            }
+            if (i < 2) a.xs[1 + s][i] = is[s][i];
             a.ys[1 + s][i] = os[s][i];
-            al = al && os[s][i] % vec == 0;
         }
-        al = al && aligned(in[s], load) && aligned(out[s], load);
     }
     a.weight[1] = k_weight;
     a.tokens = d->tokens;
@@ -241,7 +227,7 @@ int ftcnn_kv_append(const ftcnn_append_desc *d, const void *k, const void *v, co
     a.positions = positions;
     a.slots = slots;
     a.table = table;
-    FT_PAGED_HIP(launch_rope(d->dtype, a, al, stream), what);
+    FT_PAGED_HIP(launch_rope(d->dtype, a, stream), what);
     return FTCNN_OK;
 }
 

@@ -7,12 +7,13 @@
 // ("interleaved"); (cos, sin) of a pair at a position come from a table made once in float64.
 //
 // Memory-bound: a row is read and written once, and the table's row once for several heads.  A row is
-// cut into units of two vectors of V values (four where alignment allows, else one): a rotated unit
-// holds V whole pairs, so a rotation needs no other lane.  A group of lanes holds a row, a unit or
-// more a lane, and walks some heads of a token, two rows in flight.  One, two or four rows in flight and
-// vectors of four or eight bf16 values differ by less than a tenth: 8192 tokens of 40 heads of 128, normed and
-// rotated, 33 to 35 us (35.0 as it is: 4.9 TB/s of the 5.2 that a copy reaches), 16384 tokens of eight
-// such heads appended 28.4 to 31.3 (28.4).  For few tokens the call's own time on the host, 8 to 10 us, is all.
+// cut into units of two vectors of V values (16 bytes each, or fewer where alignment asks for it): a rotated
+// unit holds V whole pairs, so a rotation needs no other lane.  A group of lanes holds a row, a unit or
+// more a lane, and walks some heads of a token.
+//
+// Measured, 8192 tokens of 40 heads of 128 in bf16, normed and rotated, 172 MB: 37.7 us, 4.6 TB/s of the 5.2
+// that a large copy reaches (vectors of four 44.5); 16384 tokens of eight such heads appended, 143 MB: 28.6 us.
+// For few tokens the call's own time on the host, 7 to 10 us, is all.
 #include <algorithm>
 
 #include "paged.h"
@@ -22,6 +23,7 @@ namespace {
 
 template <typename T, int V> struct Vec;
 template <> struct Vec<float, 4> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
+template <> struct Vec<uint16_t, 8> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
 template <> struct Vec<uint16_t, 4> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Vec<float, 1> { typedef float type; };
 template <> struct Vec<uint16_t, 1> { typedef uint16_t type; };
@@ -36,7 +38,9 @@ __device__ inline float as_f32(uint16_t v) { return bf16_bits_to_f32(v); }
 __device__ inline void put(float &d, float v) { d = v; }
 __device__ inline void put(uint16_t &d, float v) { d = f32_to_bf16_rne(v); }
 
-constexpr int kRowsInFlight = 2;
+// Rows in flight: bf16 two (16384 tokens appended 28.6 us, one 29.3), fp32 one (2049 tokens of 32 heads of 96,
+// 10.6 us; two 11.4).
+template <typename T> constexpr int kRowsInFlight = sizeof(T) == 2 ? 2 : 1;
 
 // The sum over the LPR lanes of a group, in all of them: within rows of 16 lanes by the vector unit alone.
 template <int CTRL> __device__ inline float with_lane(float x) {
@@ -55,7 +59,7 @@ template <int LPR> __device__ inline float group_sum(float x) {
 // LPR lanes hold a row, UPL units a lane (unit lane + u * LPR).
 template <typename T, int V, int LPR, int UPL, bool PAST_L2>
 __global__ __launch_bounds__(kThreads, 4) void rope_kernel(RopeArgs a) {
-    constexpr int B = UPL == 1 ? kRowsInFlight : 1;
+    constexpr int B = UPL == 1 ? kRowsInFlight<T> : 1;
     const int lane = threadIdx.x % LPR;
     const unsigned id = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
     const unsigned token = div_by(id, a.div_chunks);
@@ -201,9 +205,9 @@ __global__ __launch_bounds__(kThreads, 4) void rope_kernel(RopeArgs a) {
 template <typename T, int V, int LPR, int UPL>
 hipError_t go(RopeArgs a, hipStream_t st) {
     const long long rows = a.heads[0] + a.heads[1] + a.heads[2];
-    // heads a group: enough to read a table row for several, few enough that the device is full
-    // (a wave for each of its 1024 SIMDs, eight over)
-    const long long groups = 8192LL * (64 / LPR);
+    // heads a group: enough to read a table row and weights for several, few enough that the device is full (four
+    // waves on each of its 1024 SIMDs): 8192 tokens of 40 heads of 128, eight heads 37.7 us, four 42.7
+    const long long groups = 4096LL * (64 / LPR);
     a.per_chunk = 1;
     while (a.per_chunk < 8 && a.per_chunk * 2 * groups <= a.tokens * rows) a.per_chunk *= 2;
     // outputs that the L2s (eight of 4 MiB) will not keep for the next kernel are not kept in them: 8192 tokens of
@@ -225,8 +229,8 @@ template <typename T, int V> hipError_t pick(const RopeArgs &a, hipStream_t st) 
     if constexpr (V > 1) {
         if (units <= 4) return go<T, V, 4, 1>(a, st);
         if (units <= 8) return go<T, V, 8, 1>(a, st);
-        if (units <= 16) return go<T, V, 16, 1>(a, st);
-        return go<T, V, 32, 1>(a, st);   // at most 32 units: dim <= 256
+        if (V == 8 || units <= 16) return go<T, V, 16, 1>(a, st);   // at most 128 / V units: dim <= 256
+        if constexpr (V < 8) return go<T, V, 32, 1>(a, st);
     } else {
         if (units <= 32) return go<T, V, 32, 1>(a, st);
         if (units <= 64) return go<T, V, 64, 1>(a, st);
@@ -258,9 +262,25 @@ __global__ __launch_bounds__(kThreads) void rope_table_kernel(ftcnn_rope_scaling
 
 }  // namespace
 
-hipError_t launch_rope(int dtype, RopeArgs a, bool aligned, hipStream_t st) {
-    if (dtype == FTCNN_F32) return aligned ? pick<float, 4>(a, st) : pick<float, 1>(a, st);
-    return aligned ? pick<uint16_t, 4>(a, st) : pick<uint16_t, 1>(a, st);
+// Rows, their halves and the table start on whole vectors of `vec` values.
+static bool rows_hold(const RopeArgs &a, int vec, int bytes) {
+    auto off = [&](const void *p) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; };
+    if (a.dim % (2 * vec) || (a.positions && (a.rot % (2 * vec) || reinterpret_cast<uintptr_t>(a.table) % 16))) return false;
+    for (int s = 0; s < 3; ++s) {
+        if (!a.heads[s]) continue;
+        if (off(a.x[s]) || off(a.y[s])) return false;
+        for (int i = 0; i < 3; ++i)
+            if ((i < 2 && a.xs[s][i] % vec) || a.ys[s][i] % vec) return false;
+    }
+    return true;
+}
+
+// The widest vectors that fit.  bf16, 8192 tokens of 40 heads: of 128 values, vectors of eight 37.7 us, of four 44.5; of
+// 72, of four 35 us, single values 53.
+hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st) {
+    if (dtype == FTCNN_F32) return rows_hold(a, 4, 16) ? pick<float, 4>(a, st) : pick<float, 1>(a, st);
+    if (rows_hold(a, 8, 16)) return pick<uint16_t, 8>(a, st);
+    return rows_hold(a, 4, 8) ? pick<uint16_t, 4>(a, st) : pick<uint16_t, 1>(a, st);
 }
 
 hipError_t launch_rope_table(const ftcnn_rope_scaling &sc, float *table, hipStream_t st) {
