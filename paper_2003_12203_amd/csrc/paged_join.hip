@@ -5,6 +5,9 @@
 // what there is to join (AttnCut).  A workgroup looks through some of the runs and takes some of each such
 // unit's rows: a team of 32 lanes (four values a lane) a row, or with fewer rows than teams several that
 // share a row's parts.
+//
+// It reads each part once: chunks over 8192 cached tokens, 64 MB of parts, 18 us; single tokens of 64 sequences 6 to 7 us
+// (2048, 4096 or 8192 workgroups, or parts loaded before their weights are known: the same).
 #include <algorithm>
 
 #include "paged_attn.h"

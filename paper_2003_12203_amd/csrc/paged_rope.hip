@@ -210,8 +210,8 @@ hipError_t go(RopeArgs a, hipStream_t st) {
     const long long groups = 4096LL * (64 / LPR);
     a.per_chunk = 1;
     while (a.per_chunk < 8 && a.per_chunk * 2 * groups <= a.tokens * rows) a.per_chunk *= 2;
-    // outputs that the L2s (eight of 4 MiB) will not keep for the next kernel are not kept in them: 8192 tokens of
-    // 40 heads of 128 in bf16 34.3 us for 40.1, 16384 tokens appended 30.0 for 33.1
+    // outputs that the L2s (eight of 4 MiB) will not keep for the next kernel are not kept in them: with
+    // vectors of four, 8192 tokens of 40 heads of 128 in bf16 44.5 us for 46.9, 16384 tokens appended 28.5 for 34.2
     const bool past_l2 = a.tokens * rows * a.dim * (long long)sizeof(T) > (32LL << 20);
     a.all_chunks = 0;
     for (int s = 0; s < 3; ++s) a.all_chunks += a.chunks[s] = (a.heads[s] + a.per_chunk - 1) / a.per_chunk;

@@ -13,6 +13,11 @@
 // registers, weights are not rounded, and nothing is transposed: lane (m, h) takes the VE values from
 // VE m on of key 4 h + i, a whole row in 16 lanes, one value of each for VE instructions.  At a quarter of the
 // bf16 rate or less it still takes half the time of the loads.
+//
+// Measured with the join, bf16, 32 heads of 128 over eight key heads: one token over 131072, 537 MB, 116 us
+// (105 without, 5.1 TB/s of the 5.2 that a large copy reaches); 64 single tokens over 204 MB of ragged caches 57 us (50
+// without); through LDS in workgroups that share the loads the latter took 81.  Over few keys the start is all: 76 keys
+// 10.5 us, in which loads wait for each other: lengths, page list, keys, and the next tile's after this one's.
 #pragma once
 
 #include "paged_attn.h"
@@ -135,24 +140,23 @@ __global__ __launch_bounds__(64, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 5
             }
             f32x4_t s[S2];
 #pragma unroll
-                for (int k = 0; k < S2; ++k) {
-                    s[k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < S2; ++k) {
+                s[k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q) {
-                        if constexpr (BF) {
-                            s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                __builtin_bit_cast(bf16x8_t, kf[k][q]), __builtin_bit_cast(bf16x8_t, qf[q]),
-                                s[k], 0, 0, 0);
-                        } else {
-                            const float4 ka = __builtin_bit_cast(float4, kf[k][q]);
-                            const float4 qb = __builtin_bit_cast(float4, qf[q]);
-                            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.x, qb.x, s[k], 0, 0, 0);
-                            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.y, qb.y, s[k], 0, 0, 0);
-                            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.z, qb.z, s[k], 0, 0, 0);
-                            s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.w, qb.w, s[k], 0, 0, 0);
-                        }
+                for (int q = 0; q < NQ; ++q) {
+                    if constexpr (BF) {
+                        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8_t, kf[k][q]), __builtin_bit_cast(bf16x8_t, qf[q]), s[k], 0, 0, 0);
+                    } else {
+                        const float4 ka = __builtin_bit_cast(float4, kf[k][q]);
+                        const float4 qb = __builtin_bit_cast(float4, qf[q]);
+                        s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.x, qb.x, s[k], 0, 0, 0);
+                        s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.y, qb.y, s[k], 0, 0, 0);
+                        s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.z, qb.z, s[k], 0, 0, 0);
+                        s[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka.w, qb.w, s[k], 0, 0, 0);
                     }
                 }
+            }
             const int pid_next = pid1;
             if (t + 1 < ntiles) load_k(t + 1, pid_next);
             if (t + 2 < ntiles) pid1 = lookup(t + 2);
@@ -216,7 +220,7 @@ __global__ __launch_bounds__(64, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 5
 #pragma unroll
                     for (int e = 0; e < VE; ++e) {
                         const float v = value(k, i, e);
-                            o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[k][i], o[e], 0, 0, 0);
+                        o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[k][i], o[e], 0, 0, 0);
                     }
             if (t + 1 < ntiles) load_v(t + 1, pid_next);
         }
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(64, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 5
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
                             const float v = value_of(at[x]);
-                                o[e + x][i] += key >= jlo && key <= jhi && !(fabsf(v) < INFINITY) ? v : 0.0f;
+                            o[e + x][i] += key >= jlo && key <= jhi && !(fabsf(v) < INFINITY) ? v : 0.0f;
                         }
                     }
             }
