@@ -166,8 +166,11 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
         ko = k_out.stride()
     if not qi[2] == qo[2] == ki[2] == ko[2] == 1:
         _bad(what, "the last dimension of queries, keys and outputs must be contiguous")
-    desc = _ROPE.pack(_DTYPE[dtype], tokens, heads, kv_heads, dim, rot, lay, max_pos, wd, eps, qi[0], qi[1], ki[0],
-                      ki[1], qo[0], qo[1], ko[0], ko[1])
+    try:
+        desc = _ROPE.pack(_DTYPE[dtype], tokens, heads, kv_heads, dim, rot, lay, max_pos, wd, eps, qi[0], qi[1], ki[0],
+                          ki[1], qo[0], qo[1], ko[0], ko[1])
+    except (struct.error, OverflowError) as e:
+        _bad(what, f"a number that its field does not hold: {e}")
     rc = _lib.load().ftcnn_qk_norm_rope(
         desc, None if q is None else q.data_ptr(), None if k is None else k.data_ptr(),
         None if positions is None else positions.data_ptr(), None if table is None else table.data_ptr(),
@@ -206,8 +209,11 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: 
     ks, vs, kc, vc = k.stride(), v.stride(), k_cache.stride(), v_cache.stride()
     if not ks[2] == vs[2] == kc[3] == vc[3] == 1:
         _bad(what, "the last dimension of keys, values and caches must be contiguous")
-    desc = _APPEND.pack(_DTYPE[dtype], tokens, kv_heads, dim, rot, lay, max_pos, wd, cache[0], cache[1], eps, 0,
-                        ks[0], ks[1], vs[0], vs[1], kc[0], kc[1], kc[2], vc[0], vc[1], vc[2])
+    try:
+        desc = _APPEND.pack(_DTYPE[dtype], tokens, kv_heads, dim, rot, lay, max_pos, wd, cache[0], cache[1], eps, 0,
+                            ks[0], ks[1], vs[0], vs[1], kc[0], kc[1], kc[2], vc[0], vc[1], vc[2])
+    except (struct.error, OverflowError) as e:
+        _bad(what, f"a number that its field does not hold: {e}")
     rc = _lib.load().ftcnn_kv_append(
         desc, k.data_ptr(), v.data_ptr(), None if positions is None else positions.data_ptr(),
         None if table is None else table.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
@@ -265,9 +271,12 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     qs, os, kc, vc = q.stride(), out.stride(), k_cache.stride(), v_cache.stride()
     if not qs[2] == os[2] == kc[3] == vc[3] == 1:
         _bad(what, "the last dimension of queries, caches and outputs must be contiguous")
-    desc = _ATTENTION.pack(_DTYPE[dtype], batch, tokens, heads, cache[2], dim, cache[0], cache[1], entries, causal,
-                           window, max_q, max_kv, dim ** -0.5 if scale is None else scale, qs[0], qs[1], os[0], os[1],
-                           kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], page_list.stride(0))
+    try:
+        desc = _ATTENTION.pack(_DTYPE[dtype], batch, tokens, heads, cache[2], dim, cache[0], cache[1], entries, causal,
+                               window, max_q, max_kv, dim ** -0.5 if scale is None else scale, qs[0], qs[1], os[0], os[1],
+                               kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], page_list.stride(0))
+    except (struct.error, OverflowError) as e:
+        _bad(what, f"a number that its field does not hold: {e}")
     L = _lib.load()
     need = L.ftcnn_paged_attention_workspace_bytes(desc)
     room = None

@@ -230,3 +230,31 @@ def test_the_example(dtype):
     worst, corrected = example().serve(dtype, new=5)
     assert worst < (0.5 if dtype == "bf16" else 1e-3)
     assert corrected >= 8   # one a step: three steps of prompts, five of single tokens and more
+
+
+@pytest.mark.parametrize("dtype,dim,rot,layout", [
+    ("bf16", 128, 128, "half"), ("bf16", 128, 24, "half"), ("bf16", 72, 72, "interleaved"), ("bf16", 96, 90, "half"),
+    ("f32", 128, 64, "interleaved"), ("f32", 80, 32, "half"), ("f32", 60, 20, "half")])
+def test_norms_and_rotation_of_many_tokens(dtype, dim, rot, layout):
+    """Several heads to a lane group and outputs past the L2s, in vectors of every width."""
+    rng = np.random.default_rng([dim, rot])
+    tokens, heads, kv = 1201, 120, 24
+    qkv = torch.from_numpy(rng.standard_normal((tokens, heads + kv, dim)).astype(np.float32)).to("cuda", DT[dtype])
+    pos = torch.from_numpy(rng.permutation(tokens).astype(np.int32)).cuda()
+    table, w = paged.rope_table(tokens, rot), torch.from_numpy(rng.random((2, dim)).astype(np.float32) + 0.5).cuda()
+    q, k = paged.qk_norm_rope(qkv[:, :heads], qkv[:, heads:], pos, table, w[0], w[1], layout=layout)
+    for got, x, weight in ((q, qkv[:, :heads], w[0]), (k, qkv[:, heads:], w[1])):
+        want, bound = sv.norm_rope(f64(x), pos.cpu().numpy(), f64(table), f64(weight), layout=layout, dtype=dtype)
+        assert (np.abs(f64(got) - want) <= bound).all()
+
+
+def test_numbers_that_do_not_fit_are_refused():
+    s = step(13, "f32", [1], [20])
+    q = s["qkv"][:, :s["heads"]]
+    args = (q, s["cache"].k, s["cache"].v, s["page_list"], s["kv_lens"])
+    with pytest.raises(ft.FtcnnError, match="does not hold"):
+        paged.paged_attention(*args, max_kv=1 << 40)
+    with pytest.raises(ft.FtcnnError, match="does not hold"):
+        paged.paged_attention(*args, scale=1e300)
+    with pytest.raises(ft.FtcnnError, match="does not hold"):
+        paged.qk_norm_rope(q, None, eps=1e300)
