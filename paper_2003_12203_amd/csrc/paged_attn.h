@@ -153,38 +153,49 @@ __device__ __forceinline__ long long divide(long long a, long long b) {
 // The even schedule: the run (of the units' costs) a workgroup takes, and where a sequence's units begin.
 struct AttnRuns {
     long long total, run;
+    long long upto;   // the work of the sequences up to this lane's, of the first 64: the whole of them mostly
+    __device__ static long long scan(const AttnArgs &a, int rows, int b) {
+        const int lane = threadIdx.x & 63;
+        long long incl = b < a.batch ? AttnSeq(a, b, rows).work(a) : 0;
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) {
+            const long long v = __shfl_up(incl, x);
+            if (lane >= x) incl += v;
+        }
+        return incl;
+    }
     // by a whole wave
     __device__ AttnRuns(const AttnArgs &a, int rows) {
         const int lane = threadIdx.x & 63;
-        long long sum = 0;
-        for (int b = lane; b < a.batch; b += 64) sum += AttnSeq(a, b, rows).work(a);
+        upto = scan(a, rows, lane);
+        long long sum = __shfl(upto, 63);
+        if (a.batch > 64) {
+            long long more = 0;
+            for (int b = 64 + lane; b < a.batch; b += 64) more += AttnSeq(a, b, rows).work(a);
 #pragma unroll
-        for (int x = 32; x > 0; x /= 2) sum += __shfl_xor(sum, x);
+            for (int x = 32; x > 0; x /= 2) more += __shfl_xor(more, x);
+            sum += more;
+        }
         total = uniform(sum);
         run = max(divide(total + a.groups - 1, a.groups), (long long)a.min_run);
     }
     // the sequence that cost `at` < total belongs to, and where that sequence begins
-    __device__ static int find(const AttnArgs &a, int rows, long long at, long long &base) {
+    __device__ int find(const AttnArgs &a, int rows, long long at, long long &base) const {
         const int lane = threadIdx.x & 63;
         base = 0;
         for (int b0 = 0;; b0 += 64) {
-            const long long mine = b0 + lane < a.batch ? AttnSeq(a, b0 + lane, rows).work(a) : 0;
-            long long incl = mine;
-#pragma unroll
-            for (int x = 1; x < 64; x *= 2) {
-                const long long v = __shfl_up(incl, x);
-                if (lane >= x) incl += v;
-            }
+            const long long incl = b0 == 0 ? upto : scan(a, rows, b0 + lane);
             const unsigned long long past = __ballot(base + incl > at);
             if (past || b0 + 64 >= a.batch) {
                 const int at_lane = past ? __builtin_ctzll(past) : 63;
-                base += __shfl(incl - mine, at_lane);
+                base += at_lane > 0 ? __shfl(incl, max(at_lane - 1, 0)) : 0;
                 return min(b0 + at_lane, a.batch - 1);
             }
             base += __shfl(incl, 63);
         }
     }
 };
+
 // Values that a row must not take up: a key that it does not see has weight zero, but zero times an infinity or NaN is
 // NaN.  Tiles that some row does not see all of are searched for such values, which are set to zero in them; a unit
 // that had any gets them back at its end, added to the rows that see them.  Their weights, whatever they
@@ -255,7 +266,7 @@ __device__ __forceinline__ void attn_schedule(const AttnArgs &a, int rows, int k
             return;
         }
         long long base;
-        int b = uniform(AttnRuns::find(a, rows, at, base));
+        int b = uniform(runs.find(a, rows, at, base));
         base = uniform(base);
         while (at < end) {
             AttnSeq sq(a, b, rows);

@@ -258,3 +258,24 @@ def test_numbers_that_do_not_fit_are_refused():
         paged.paged_attention(*args, scale=1e300)
     with pytest.raises(ft.FtcnnError, match="does not hold"):
         paged.qk_norm_rope(q, None, eps=1e300)
+
+
+@pytest.mark.parametrize("new", [1, 9])
+def test_more_sequences_than_lanes(new):
+    """The schedule over 150 ragged sequences, some of them empty, and the cut units among them."""
+    rng = np.random.default_rng(new)
+    length = [int(n) for n in rng.integers(new, 700, 150)]
+    length[3] = length[64] = length[149] = 0
+    length[70] = 6000
+    news = [min(new, n) if b % 7 else 0 for b, n in enumerate(length)]
+    news[70] = new
+    s = step(14, "bf16", news, length, heads=4, kv=2)
+    out = run(s)
+    lse = torch.empty(sum(news), 4, device="cuda")
+    run(s, lse=lse)
+    h = s["heads"]
+    q, _ = paged.qk_norm_rope(s["qkv"][:, :h], None, s["positions"], s["table"], s["weight"])
+    want, wl, bo, bl = sv.attention(f64(q), f64(s["cache"].k), f64(s["cache"].v), s["page_list"].cpu().numpy(), length,
+                                    s["q_starts"].cpu().numpy(), dtype="bf16")
+    assert (np.abs(f64(out) - want) <= bo).all()
+    assert (np.abs(f64(lse) - wl) <= bl).all()
