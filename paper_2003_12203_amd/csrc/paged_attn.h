@@ -774,22 +774,27 @@ __global__ __launch_bounds__(64 * WR, DP > 128 || sizeof(T) * DP > 256 ? 1 : 2) 
     attn_schedule<EVEN>(a, L::ROWS, L::KEYS, unit);
 }
 
-template <typename T, int DP, int WR, int KS> hipError_t attn_go(const AttnArgs &a, hipStream_t st) {
+template <typename T, int DP, int WR, int KS, bool EVEN, bool ONE>
+hipError_t attn_launch(const AttnArgs &a, unsigned blocks, hipStream_t st) {
     using L = AttnTile<T, DP, WR, KS>;
-    auto launch = [&](auto kernel, unsigned blocks) {
+    auto kernel = attn_kernel<T, DP, WR, KS, EVEN, ONE>;
+    if constexpr (L::LDS > 65536) {
         static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                            hipFuncAttributeMaxDynamicSharedMemorySize, L::LDS);
         if (attr != hipSuccess) return attr;
-        kernel<<<blocks, L::THREADS, L::LDS, st>>>(a);
-        return hipGetLastError();
-    };
-    const bool one = a.page % (L::KEYS / WR) == 0 && std::max(a.kb[1], a.vb[1]) < 1u << 24;
+    }
+    kernel<<<blocks, L::THREADS, L::LDS, st>>>(a);
+    return hipGetLastError();
+}
+template <typename T, int DP, int WR, int KS> hipError_t attn_go(const AttnArgs &a, hipStream_t st) {
+    // page addresses in scalars (two prompts of 8192 tokens 1034 us, with an address a lane 1102)
+    const bool one = a.page % (AttnTile<T, DP, WR, KS>::KEYS / WR) == 0 && std::max(a.kb[1], a.vb[1]) < 1u << 24;
     const unsigned whole = (unsigned)a.tiles * a.kv_heads * a.batch;
     if (a.groups)
-        return one ? launch(attn_kernel<T, DP, WR, KS, true, true>, a.groups)
-                   : launch(attn_kernel<T, DP, WR, KS, true, false>, a.groups);
-    return one ? launch(attn_kernel<T, DP, WR, KS, false, true>, whole)
-               : launch(attn_kernel<T, DP, WR, KS, false, false>, whole);
+        return one ? attn_launch<T, DP, WR, KS, true, true>(a, a.groups, st)
+                   : attn_launch<T, DP, WR, KS, true, false>(a, a.groups, st);
+    return one ? attn_launch<T, DP, WR, KS, false, true>(a, whole, st)
+               : attn_launch<T, DP, WR, KS, false, false>(a, whole, st);
 }
 
 }  // namespace ftcnn
