@@ -69,7 +69,7 @@ AttnPlan attn_plan(const ftcnn_attention_desc &d) {
     p.tiles = (int)((rows + tile - 1) / tile);
     // workgroups that are on the device at a time (registers and LDS)
     const bool narrow = p.dp * es <= 256;
-    const long long fit = kComputeUnits * (wide ? (narrow ? 2 : 1) : (narrow ? 8 : 4));
+    const long long fit = kComputeUnits * (wide ? (p.dp <= 128 ? 2 : 1) : (narrow ? 8 : 4));
     const long long some = std::min<long long>((long long)d.batch * p.tiles, d.tokens * group / tile + d.batch);
     const long long units = some * d.kv_heads;
     const long long range = d.window > 0 ? std::min<long long>(max_kv, d.window + tile / group + 1) : max_kv;
@@ -84,8 +84,9 @@ AttnPlan attn_plan(const ftcnn_attention_desc &d) {
     const long long rest = wide ? (bf ? 1100 : 330) : 200;
     const long long mean = d.window > 0 || !d.causal ? range : std::max(1LL, max_kv - max_q / 2);
     const long long whole = std::max(range, units * mean / fit) + p.unit_cost * ((units + fit - 1) / fit);
-    // as many runs on every compute unit: 365 on 256 of them 53 us, 256 runs 42
-    long long runs = std::min(fit, (units * range + p.min_run - 1) / p.min_run);
+    // as many runs on every compute unit: 365 on 256 of them 53 us, 256 runs 42; fp32 workgroups, whose matrix
+    // instructions leave a second one nothing, one each: 200 tokens over 6000, heads of 128, 125 us, two 138
+    long long runs = std::min(wide && !bf ? kComputeUnits : fit, (units * range + p.min_run - 1) / p.min_run);
     if (runs > kComputeUnits) runs -= runs % kComputeUnits;
     const long long even = units * (mean + p.unit_cost) / runs + rest;
     if (even < whole) {

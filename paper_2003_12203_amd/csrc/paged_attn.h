@@ -31,7 +31,8 @@
 // 1050 us, 1050 TFLOP/s of the 1260 that a product of 8192 x 8192 matrices reaches; a rise of the matrix cores' share
 // from 45 to 55 % took the clock from 2.13 to 1.87 GHz, so the power limit is near as well.  Chunks over 8192 cached tokens
 // take twice their floor: the cut units' parts are written, read and joined (64 MB), and a workgroup's start is
-// five tiles long.  fp32, a prompt of 2048 tokens: 102 TFLOP/s of 153.
+// five tiles long.  fp32, a prompt of 4096 tokens: 103 TFLOP/s of 153
+// with heads of 64, 115 with 128.
 #pragma once
 
 #include <limits.h>
@@ -588,8 +589,9 @@ template <typename T, int DP, int KS> struct AttnRows {
     }
 };
 
+// Two workgroups to a compute unit where registers hold them (fp32, heads of 128, a prompt of 4096 tokens: 597 us, one 1037).
 template <typename T, int DP, int WR, int KS, bool EVEN, bool ONE>
-__global__ __launch_bounds__(64 * WR, DP > 128 || sizeof(T) * DP > 256 ? 1 : 2) void attn_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * WR, DP > 128 ? 1 : 2) void attn_kernel(AttnArgs a) {
     using L = AttnTile<T, DP, WR, KS>;
     constexpr int UPR = L::UPR, EU = L::EU, RB = L::RB, OWN = L::KEYS / WR, STEP = 64 / UPR;   // rows of a wave's loads, of one
     extern __shared__ __align__(1024) unsigned char lds[];
