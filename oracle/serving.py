@@ -87,7 +87,8 @@ def attention(q, k_cache, v_cache, page_list, kv_lens, q_starts=None, scale=None
     bo, bl = np.zeros(q.shape), np.zeros(q.shape[:2])
     u_p = U_OUT["bf16"] if dtype == "bf16" else U32   # the weights as the product takes them
     for b, n in enumerate(kv_lens):
-        lo, hi = (b, b + 1) if q_starts is None else (q_starts[b], q_starts[b + 1])
+        n = int(n)
+        lo, hi = (b, b + 1) if q_starts is None else (int(q_starts[b]), int(q_starts[b + 1]))
         rows = [(int(page_list[b][j // page]), j % page) for j in range(n)]
         for h in range(kv_heads):
             K = np.array([k_cache[r][h] for r in rows], np.float64).reshape(n, dim)

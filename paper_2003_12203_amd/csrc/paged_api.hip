@@ -296,7 +296,9 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
     a.page = d->page;
     a.capacity = d->list_len * d->page;
     a.causal = d->causal != 0;
-    a.window = d->window;
+    // no sequence holds more than the list can name: a wider window hides nothing more, and sums of positions
+    // and windows of at most 2^30 stay within 32 bits
+    a.window = std::min(d->window, a.capacity);
     a.tiles = pl.tiles;
     a.groups = pl.groups;
     a.min_run = pl.min_run;
