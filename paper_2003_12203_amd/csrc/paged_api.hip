@@ -14,7 +14,9 @@ namespace {
         if (_e != hipSuccess) return set_error(FTCNN_E_HIP, "%s: %s", where, hipGetErrorString(_e)); \
     } while (0)
 
-constexpr long long kMaxRows = 1LL << 30;   // rows a sequence's page list can name, and rows of queries
+// Rows a sequence's page list can name, rows of queries, key heads of all sequences.  attn_plan's products of units
+// and keys then stay below 2^63.
+constexpr long long kMaxRows = 1LL << 30;
 
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -53,6 +55,7 @@ int check_rope(const char *what, int32_t dtype, int32_t tokens, int32_t heads, i
 
 AttnPlan attn_plan(const ftcnn_attention_desc &d) {
     AttnPlan p{};
+    if (d.batch == 0 || d.tokens == 0) return p;   // no units
     const long long group = d.heads / d.kv_heads, capacity = (long long)d.list_len * d.page;
     const long long max_q = std::max(1LL, std::min<long long>(d.max_q > 0 ? d.max_q : d.tokens, d.tokens));
     const long long max_kv = std::max(1LL, std::min(d.max_kv > 0 ? d.max_kv : capacity, capacity));
@@ -118,6 +121,8 @@ int check_attention(const ftcnn_attention_desc *d) {
         return set_error(FTCNN_E_UNSUPPORTED, "%s: dim %d (a multiple of 8, at most 256)", what, d->dim);
     if ((long long)d->tokens * d->heads > kMaxRows || (long long)d->list_len * d->page > kMaxRows)
         return set_error(FTCNN_E_SHAPE, "%s: more than 2^30 rows", what);
+    if ((long long)d->batch * d->kv_heads > kMaxRows)
+        return set_error(FTCNN_E_SHAPE, "%s: %d sequences of %d key heads", what, d->batch, d->kv_heads);
     if (d->window < 0 || (d->window > 0 && !d->causal))
         return set_error(FTCNN_E_ARG, "%s: window %d (0, or positive with causal)", what, d->window);
     if (!(d->scale > 0.0f) || !std::isfinite(d->scale))
@@ -233,7 +238,7 @@ int ftcnn_kv_append(const ftcnn_append_desc *d, const void *k, const void *v, co
 }
 
 size_t ftcnn_paged_attention_workspace_bytes(const ftcnn_attention_desc *desc) {
-    return check_attention(desc) == FTCNN_OK && desc->tokens > 0 ? attn_plan(*desc).bytes : 0;
+    return check_attention(desc) == FTCNN_OK ? attn_plan(*desc).bytes : 0;
 }
 
 int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const void *k_cache, const void *v_cache,
