@@ -503,7 +503,8 @@ typedef struct {
  * lies in row j % page of page page_list[b][j / page].
  *   out = sum_j softmax_j(scale q . k_j) v_j,   lse = log sum_j exp(scale q . k_j)
  * with lse (fp32 [tokens][heads], NULL: not wanted) the natural logarithm.  A row that sees
- * nothing (an empty cache, or fewer cached tokens than new ones) is 0, its lse -infinity.
+ * nothing (an empty cache, or fewer cached tokens than new ones) is 0, its lse -infinity; so are
+ * rows of no sequence, before q_starts[0] and from q_starts[batch] on (padding).
  * Scores, maxima, sums and outputs are held in fp32; bf16 calls round the softmax weights,
  * relative to a maximum, to bf16 for the product with the values.
  * kv_lens are taken within [0, list_len * page], q_starts within [0, tokens], and a page number

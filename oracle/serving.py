@@ -77,13 +77,13 @@ def append(k_cache, v_cache, k, v, slots):
 
 
 def attention(q, k_cache, v_cache, page_list, kv_lens, q_starts=None, scale=None, causal=True, window=0, dtype="f32"):
-    """-> (out, lse, bound of out, bound of lse); tokens of no sequence are NaN."""
+    """-> (out, lse, bound of out, bound of lse); tokens of no sequence are 0, their lse -inf."""
     q = np.asarray(q, np.float64)
     tokens, heads, dim = q.shape
     page, kv_heads = k_cache.shape[1:3]
     group = heads // kv_heads
     scale = 1.0 / np.sqrt(dim) if scale is None else scale
-    out, lse = np.full(q.shape, np.nan), np.full(q.shape[:2], np.nan)
+    out, lse = np.zeros(q.shape), np.full(q.shape[:2], -np.inf)
     bo, bl = np.zeros(q.shape), np.zeros(q.shape[:2])
     u_p = U_OUT["bf16"] if dtype == "bf16" else U32   # the weights as the product takes them
     for b, n in enumerate(kv_lens):

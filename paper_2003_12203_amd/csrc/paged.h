@@ -87,6 +87,7 @@ AttnPlan attn_plan(const ftcnn_attention_desc &d);
 hipError_t launch_attn_bf16(const AttnPlan &pl, const AttnArgs &a, hipStream_t st);
 hipError_t launch_attn_f32(const AttnPlan &pl, const AttnArgs &a, hipStream_t st);
 hipError_t launch_attn_join(int dtype, const AttnPlan &pl, const AttnArgs &a, hipStream_t st);
+hipError_t launch_attn_clear(int dtype, const AttnArgs &a, hipStream_t st);   // a batch of no sequences
 
 // Records the text of ftcnn_last_error() and returns `code`.
 int set_error(int code, const char *fmt, ...);

@@ -249,8 +249,8 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
     if (rc != FTCNN_OK) return rc;
     if (!q_starts && d->tokens != d->batch)
         return set_error(FTCNN_E_SHAPE, "%s: %d tokens of %d sequences need q_starts", what, d->tokens, d->batch);
-    if (d->tokens == 0 || d->batch == 0) return FTCNN_OK;
-    if (!q || !k_cache || !v_cache || !kv_lens || !out || (!page_list && d->list_len))
+    if (d->tokens == 0) return FTCNN_OK;
+    if (!out || (d->batch && (!q || !k_cache || !v_cache || !kv_lens || (!page_list && d->list_len))))
         return set_error(FTCNN_E_ARG, "%s: null pointer", what);
     const int vec = d->dtype == FTCNN_F32 ? 4 : 8;
     bool al = aligned16(q) && aligned16(k_cache) && aligned16(v_cache) && aligned16(out);
@@ -314,6 +314,10 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
     a.div_page = fast_div((uint32_t)d->page);
     a.div_group = fast_div((uint32_t)a.group);
     a.scale_log2 = d->scale * 1.44269504088896340736f;
+    if (d->batch == 0) {
+        FT_PAGED_HIP(launch_attn_clear(d->dtype, a, stream), what);
+        return FTCNN_OK;
+    }
     FT_PAGED_HIP(d->dtype == FTCNN_F32 ? launch_attn_f32(pl, a, stream) : launch_attn_bf16(pl, a, stream), what);
     if (pl.groups) FT_PAGED_HIP(launch_attn_join(d->dtype, pl, a, stream), "paged_attention: join");
     return FTCNN_OK;

@@ -307,6 +307,24 @@ __device__ __forceinline__ void store4(uint16_t *p, float4 v) {
     *reinterpret_cast<uint2 *>(p) = b.q;
 }
 
+// Rows of no sequence, before q_starts[0] and from q_starts[batch] on (padding up to a captured step's size), are what
+// rows that see nothing are: a caller's buffers hold anything.  The launch's workgroups share them.
+template <typename T, int THREADS> __device__ __forceinline__ void attn_clear_unowned(const AttnArgs &a) {
+    if (!a.q_starts) return;
+    const int first = min(max(a.q_starts[0], 0), a.tokens), last = min(max(a.q_starts[a.batch], first), a.tokens);
+    const int count = first + a.tokens - last, quads = a.dim / 4, heads = a.kv_heads * a.group;
+    for (int i = blockIdx.x; i < count; i += gridDim.x) {
+        const long long token = i < first ? i : last + (i - first);
+        T *row = static_cast<T *>(a.o) + token * a.os[0];
+        for (int x = threadIdx.x; x < heads * quads; x += THREADS) {
+            const int head = x / quads;
+            store4(row + head * a.os[1] + 4 * (x - head * quads), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+        }
+        if (a.lse)
+            for (int h = threadIdx.x; h < heads; h += THREADS) a.lse[token * heads + h] = -INFINITY;
+    }
+}
+
 template <typename T, int DP, int WR, int KS> struct AttnTile {
     static constexpr int THREADS = 64 * WR, ROWS = 32 * WR, KEYS = 32 * KS;
     static constexpr int EU = 16 / sizeof(T);          // values of a 16-byte unit
@@ -774,6 +792,7 @@ __global__ __launch_bounds__(64 * WR, DP > 128 ? 1 : 2) void attn_kernel(AttnArg
     };
 
     attn_schedule<EVEN>(a, L::ROWS, L::KEYS, unit);
+    attn_clear_unowned<T, L::THREADS>(a);
 }
 
 template <typename T, int DP, int WR, int KS, bool EVEN, bool ONE>

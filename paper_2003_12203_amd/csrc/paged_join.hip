@@ -127,7 +127,18 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, int row
     }
 }
 
+template <typename T> __global__ __launch_bounds__(kThreads) void attn_clear_kernel(AttnArgs a) {
+    attn_clear_unowned<T, kThreads>(a);
+}
+
 }  // namespace
+
+hipError_t launch_attn_clear(int dtype, const AttnArgs &a, hipStream_t st) {
+    const unsigned blocks = (unsigned)std::min(a.tokens, 2048);
+    if (dtype == FTCNN_F32) attn_clear_kernel<float><<<blocks, kThreads, 0, st>>>(a);
+    else attn_clear_kernel<uint16_t><<<blocks, kThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
 
 hipError_t launch_attn_join(int dtype, const AttnPlan &pl, const AttnArgs &a, hipStream_t st) {
     // rows of a unit to a workgroup, and workgroups to look through the runs: about 2048 in all

@@ -277,6 +277,7 @@ __global__ __launch_bounds__(64, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 5
                 sum == 0.0f ? -INFINITY : (m * c + __log2f(sum)) * 0.693147180559945309f;
     };
     attn_schedule<EVEN>(a, ROWS, KEYS, unit);
+    attn_clear_unowned<T, 64>(a);
 }
 
 template <typename T, int DP> hipError_t stream_go(const AttnArgs &a, hipStream_t st) {

@@ -229,7 +229,8 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """ftcnn_paged_attention: the new tokens q [tokens][heads][dim] of a batch of sequences over each one's
     pages (page_list int32 [batch][entries], kv_lens int32 [batch], the new tokens' rows among them).
-    q_starts int32 [batch + 1] says whose tokens are whose (None: one of each sequence).  max_q and max_kv, the
+    q_starts int32 [batch + 1] says whose tokens are whose (None: one of each sequence; tokens of no sequence are
+    0).  max_q and max_kv, the
     longest sequence's new and cached tokens where the caller knows them, size the launch.  scale defaults to
     1 / sqrt(dim).  lse (float32 [tokens][heads]) is filled when given.  workspace: uint8, 256-byte aligned;
     allocated when needed and not given."""

@@ -1,10 +1,11 @@
 """Attention over the paged cache at the ends of its arguments' ranges, against its definition in float64."""
 import numpy as np
 import pytest
+import torch
 
 import paper_2003_12203_amd as ft
 from paper_2003_12203_amd import paged
-from test_gpu_paged import batch, check
+from test_gpu_paged import DT, batch, check
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +29,31 @@ def test_windows_wider_than_any_sequence(dtype, window, new, length, split):
     args = batch(rng, new, length, 4, 1, 64, dtype, 16, fill=float("nan"))
     assert is_split(args[0], args[1], args[3], new, length, window=window) == split
     check(*args, dtype, window=window, max_q=max(new), max_kv=max(length))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new,length,split", [
+    ([200], [6000], True), ([1, 3], [6000, 20], True), ([60, 0, 20], [60, 9, 12], False), ([1, 1, 0], [9, 0, 5], False)])
+@pytest.mark.parametrize("before,after", [(0, 1), (3, 0), (2, 300)])
+def test_rows_of_no_sequence(dtype, new, length, split, before, after):
+    """Queries before the first sequence's and after the last one's: 0 and -infinity, whatever the buffers held."""
+    rng = np.random.default_rng([sum(new), before, after])
+    q, kc, vc, lists, lens, starts = batch(rng, [before, *new, after], [1, *length, 1], 4, 1, 72, dtype, 16)
+    lists, lens, starts = lists[1:-1], lens[1:-1], starts[1:-1]
+    assert is_split(q, kc, lists, new, length) == split
+    q[:before] = q[len(q) - after:] = float("nan")
+    out = torch.full((q.shape[0], 4, 80), 7.0, dtype=q.dtype, device="cuda")
+    check(q, kc, vc, lists, lens, starts, dtype, max_q=max(new), max_kv=max(length), out=out[..., :72])
+    assert (out[..., 72:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_batch_of_no_sequences(dtype):
+    kc = torch.zeros(2, 16, 2, 64, dtype=DT[dtype], device="cuda")
+    q = torch.full((5, 4, 64), float("nan"), dtype=DT[dtype], device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((5, 4), 7.0, device="cuda")
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = paged.paged_attention(q, kc, kc, none[:0].view(0, 3), none[:0], none, out=out, lse=lse)
+    assert got is out and not out.any() and torch.isneginf(lse).all()
+    with pytest.raises(ft.FtcnnError, match="q_starts"):
+        paged.paged_attention(q, kc, kc, none[:0].view(0, 3), none[:0])
