@@ -198,9 +198,11 @@ struct AttnRuns {
 };
 
 // Values that a row must not take up: a key that it does not see has weight zero, but zero times an infinity or NaN is
-// NaN.  Tiles that some row does not see all of are searched for such values, which are set to zero in them; a unit
-// that had any gets them back at its end, added to the rows that see them.  Their weights, whatever they
-// are, are positive, and neither these nor a second addition change the sum of infinities and NaN.
+// NaN.  Tiles that some row (of the workgroup, which shares them) does not see all of are searched for such values, which
+// are set to zero in them; a unit that had any gets them back at its end, added to the rows that see them, once.  In the
+// other tiles they are multiplied as they are; that one of these may get a value a second time changes nothing of
+// a sum that is infinite or NaN.  Every wave searches such a tile before it reads it, so that no result hangs on which
+// wave came first.
 template <typename T> struct NonFinite;
 template <> struct NonFinite<uint16_t> {   // two values a word: the carry of a full exponent reaches its sign
     __device__ static uint32_t find(uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; }
@@ -639,8 +641,11 @@ __global__ __launch_bounds__(64 * WR, DP > 128 ? 1 : 2) void attn_kernel(AttnArg
         const int pos = sq.kv - sq.nq + qi;
         const int jhi = min(a.causal ? pos : sq.kv - 1, k1 - 1);   // the keys it sees: jlo..jhi
         const int jlo = a.window > 0 ? pos - a.window + 1 : 0;
-        const int jhi_min = __builtin_amdgcn_readlane(jhi, 0);
-        const int jlo_max = __builtin_amdgcn_readlane(jlo, 31);
+        // Of tiles [whole0, whole1) the workgroup's first row and its last one, so all of its rows, see every key.
+        const int jhi_min = min(a.causal ? sq.kv - sq.nq + i0 : sq.kv - 1, k1 - 1);
+        const int jlo_max = a.window > 0 ? sq.kv - sq.nq + i1 - a.window + 1 : 0;
+        const int whole0 = uniform((max(jlo_max - k0, 0) + L::KEYS - 1) / L::KEYS);
+        const int whole1 = uniform(max(jhi_min + 1 - k0, 0) / L::KEYS);
         rows.start(static_cast<const T *>(a.q) + (long long)(sq.q0 + qi) * a.qs[0] + (long long)head * a.qs[1], a.dim,
                    half);
 
@@ -716,7 +721,6 @@ __global__ __launch_bounds__(64 * WR, DP > 128 ? 1 : 2) void attn_kernel(AttnArg
                         __attribute__((always_inline)) {
             wait_loads();
             tile_barrier();   // keys t + 1 and values t have landed, and nobody reads keys t or values t - 1 any more
-            const int j0 = k0 + t * L::KEYS, j1 = j0 + L::KEYS - 1;
             const unsigned char *kt = lds + ((t + 1) & 1) * L::SIDE, *vt = lds + (2 + (t & 1)) * L::SIDE;
             auto values = [&]() __attribute__((always_inline)) { issue(t + 1, vbase, a.vb, other, true); };
             auto keys = [&]() __attribute__((always_inline)) {
@@ -728,8 +732,8 @@ __global__ __launch_bounds__(64 * WR, DP > 128 ? 1 : 2) void attn_kernel(AttnArg
                 keys();
                 return;
             }
-            if (j1 > jhi_min || j0 < jlo_max) {
-                rows.mask(now, j0, jlo, jhi);
+            if (t < whole0 || t >= whole1) {   // the whole workgroup: see NonFinite
+                rows.mask(now, k0 + t * L::KEYS, jlo, jhi);
                 top = rows.peak(now);
                 if (rows.wash_tile(lds + (2 + (t & 1)) * L::SIDE) && lane == 0) {
                     atomicMin(&dirt[0], t);

@@ -5,7 +5,7 @@ import torch
 
 import paper_2003_12203_amd as ft
 from paper_2003_12203_amd import paged
-from test_gpu_paged import DT, batch, check
+from test_gpu_paged import DT, attend, batch, check
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +57,23 @@ def test_a_batch_of_no_sequences(dtype):
     assert got is out and not out.any() and torch.isneginf(lse).all()
     with pytest.raises(ft.FtcnnError, match="q_starts"):
         paged.paged_attention(q, kc, kc, none[:0].view(0, 3), none[:0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new,length,window,key", [
+    (128, 128, 0, 5),          # rows of the first wave do not see all of its tile, rows of the last do
+    (128, 2128, 0, 2005), (128, 2128, 0, 2060),
+    (128, 700, 600, 110)])     # a tile that the window leaves: the last rows do not see it
+def test_an_infinite_value_of_a_weight_below_fp32(dtype, new, length, window, key):
+    """exp(-400) is zero in fp32 and not in float64: the value is an infinity to every row that sees it, whichever of
+    the waves that share its tile looked at it first."""
+    rng = np.random.default_rng(key)
+    q, kc, vc, lists, lens, starts = batch(rng, [new], [length], 1, 1, 64, dtype, 16)
+    page, row = lists[0, key // 16], key % 16
+    q[:, :, 0] = 8.0
+    kc[page, row, 0, 0] = -400.0
+    vc[page, row, 0, 3] = float("inf")
+    first = attend(q, kc, vc, lists, lens, starts, max_q=new, max_kv=length, window=window)
+    got = check(q, kc, vc, lists, lens, starts, dtype, max_q=new, max_kv=length, window=window)
+    assert torch.equal(first[0], got[0]) and torch.equal(first[1], got[1])
+    assert torch.isposinf(got[0][:, 0, 3]).any()
