@@ -10,7 +10,8 @@ call allocates belong to that stream.
 
 Shapes: queries [tokens][heads][dim], keys and values [tokens][kv_heads][dim], caches
 [pages][page][kv_heads][dim], of float32 or bfloat16, strided as they come with ``dim`` contiguous (a
-slice of a packed projection, a cache that holds a page's heads one after the other).
+slice of a packed projection, a cache that holds a page's heads one after the other).  There are no
+backward passes: where gradients are recorded (not under ``torch.no_grad()``), a tensor that requires them is refused.
 
     table = paged.rope_table(max_pos, dim)
     cache = paged.PagedCache(pages, page, kv_heads, dim, "bf16")
@@ -44,6 +45,7 @@ _ATTENTION = struct.Struct("=13if11q")
 # (0.1 us; torch.cuda.current_stream() 2.7).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
+_recording = torch.is_grad_enabled
 
 
 def _bad(what: str, why: str):
@@ -69,6 +71,10 @@ class _On:
     def __exit__(self, *exc):
         for c in reversed(self.contexts):
             c.__exit__(*exc)
+
+
+def _no_backward(what: str):
+    _bad(what, "no backward pass: call it under torch.no_grad(), or detach the tensors that require gradients")
 
 
 def _fail(what: str, rc: int):
@@ -138,6 +144,10 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     if stream is not None or dev != _current_device():
         with _On(x.device, stream):
             return qk_norm_rope(q, k, positions, table, q_weight, k_weight, eps, layout, q_out, k_out)
+    if _recording() and (x.requires_grad or (k is not None and k.requires_grad) or
+                         (q_weight is not None and q_weight.requires_grad) or
+                         (k_weight is not None and k_weight.requires_grad)):
+        _no_backward(what)
     tokens, heads, dim = shape
     kv_heads = 0
     rot, lay, max_pos, wd = _rotation(what, dtype, tokens, dim, dev, positions, table, q_weight, k_weight, layout)
@@ -194,6 +204,9 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: 
     if stream is not None or dev != _current_device():
         with _On(k.device, stream):
             return kv_append(k, v, k_cache, v_cache, slots, positions, table, k_weight, eps, layout)
+    if _recording() and (k.requires_grad or v.requires_grad or k_cache.requires_grad or v_cache.requires_grad or
+                         (k_weight is not None and k_weight.requires_grad)):
+        _no_backward(what)
     tokens, kv_heads, dim = shape
     if not (v.dtype is dtype and v.shape == shape and v.get_device() == dev):
         _bad(what, f"v must be like k, {dtype} {tuple(shape)} on device {dev}, not {_is(v)}")
@@ -242,6 +255,8 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         with _On(q.device, stream):
             return paged_attention(q, k_cache, v_cache, page_list, kv_lens, q_starts, max_q, max_kv, scale, causal,
                                    window, out, lse, workspace)
+    if _recording() and (q.requires_grad or k_cache.requires_grad or v_cache.requires_grad):
+        _no_backward(what)
     tokens, heads, dim = shape
     cache = k_cache.shape
     if not (k_cache.dtype is dtype and len(cache) == 4 and cache[3] == dim and k_cache.get_device() == dev):

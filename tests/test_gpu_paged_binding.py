@@ -1,0 +1,59 @@
+"""What the Python binding of the serving operators refuses."""
+import pytest
+import torch
+
+import paper_2003_12203_amd as ft
+from paper_2003_12203_amd import paged
+
+pytestmark = pytest.mark.gpu
+
+
+def arguments(dtype=torch.bfloat16):
+    """One sequence of five tokens, of which three are new: (queries, keys, values, caches, arrays by name)."""
+    torch.manual_seed(0)
+    x = torch.randn(3, 8, 64, device="cuda").to(dtype)
+    cache = paged.PagedCache(2, 16, 2, 64, "bf16" if dtype is torch.bfloat16 else "f32")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    return dict(q=x[:, :4], k=x[:, 4:6], v=x[:, 6:], k_cache=cache.k, v_cache=cache.v, table=paged.rope_table(8, 64),
+                q_weight=torch.ones(64, device="cuda"), k_weight=torch.ones(64, device="cuda"),
+                positions=torch.tensor([2, 3, 4], **i32), slots=torch.tensor([18, 19, 20], device="cuda"),
+                page_list=torch.tensor([[1]], **i32), kv_lens=torch.tensor([5], **i32),
+                q_starts=torch.tensor([0, 3], **i32))
+
+
+def rope(a):
+    return paged.qk_norm_rope(a["q"], a["k"], a["positions"], a["table"], a["q_weight"], a["k_weight"])
+
+
+def append(a):
+    paged.kv_append(a["k"], a["v"], a["k_cache"], a["v_cache"], a["slots"], a["positions"], a["table"], a["k_weight"])
+
+
+def attend(a):
+    return paged.paged_attention(a["q"], a["k_cache"], a["v_cache"], a["page_list"], a["kv_lens"], a["q_starts"], 3, 5)
+
+
+@pytest.mark.parametrize("call,names", [
+    (rope, ("q", "k", "q_weight", "k_weight")), (append, ("k", "v", "k_cache", "v_cache", "k_weight")),
+    (attend, ("q", "k_cache", "v_cache"))])
+def test_gradients_are_not_dropped_silently(call, names):
+    for name in names:
+        a = arguments()
+        a[name] = a[name].detach().requires_grad_()
+        with pytest.raises(ft.FtcnnError, match="no backward"):
+            call(a)
+            pytest.fail(f"{name} that requires a gradient was not refused")
+        with torch.no_grad():
+            call(a)
+        with torch.inference_mode():
+            call(a)
+        a[name] = a[name].detach()
+        call(a)
+
+
+def test_keys_alone_and_queries_alone_that_require_gradients():
+    a = arguments()
+    k = a["k"].detach().requires_grad_()
+    for q, k in ((None, k), (k, None)):
+        with pytest.raises(ft.FtcnnError, match="no backward"):
+            paged.qk_norm_rope(q, k)
