@@ -323,6 +323,12 @@ class PagedCache:
         self.pages, self.page = pages, page
 
     def slots(self, page_list: torch.Tensor, seq: torch.Tensor, positions: torch.Tensor) -> torch.Tensor:
-        """The rows (for kv_append) of tokens at the given positions of sequences seq."""
-        p = positions.long()
-        return page_list[seq.long(), p // self.page].long() * self.page + p % self.page
+        """The rows (for kv_append) of tokens at the given positions of sequences seq; -1 (written nowhere) for padding:
+        a sequence or position outside the list."""
+        batch, entries = page_list.shape
+        p, s = positions.long(), seq.long()
+        if batch * entries == 0:
+            return torch.full_like(p, -1)
+        p_in, s_in = p.clamp(0, entries * self.page - 1), s.clamp(0, batch - 1)
+        rows = page_list[s_in, p_in // self.page].long() * self.page + p_in % self.page
+        return torch.where((p == p_in) & (s == s_in), rows, -1)

@@ -1,9 +1,10 @@
 """The serving operators' C entry points and binding at the ends of their arguments' ranges, on the host (no GPU
 needed)."""
 import pytest
+import torch
 
 import paper_2003_12203_amd as ft
-from paper_2003_12203_amd import _lib
+from paper_2003_12203_amd import _lib, paged
 from test_paged_abi import E_SHAPE, attention, call_attention
 
 
@@ -30,3 +31,21 @@ def test_more_key_heads_than_the_plan_counts_are_refused():
 def test_the_largest_sizes_have_a_plan(kw, dtype, hints):
     d = attention(dtype=dtype, list_len=2 ** 26, max_q=hints[0], max_kv=hints[1], **kw)
     assert _lib.load().ftcnn_paged_attention_workspace_bytes(bytes(d)) < 1 << 32
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_rows_of_padding_are_nowhere(dtype):
+    """Positions and sequences outside the list have no row: no other token's either."""
+    cache = paged.PagedCache(6, 4, 2, 8, "f32", device="cpu")
+    lists = torch.tensor([[5, 1, 0], [2, 3, 4]], dtype=torch.int32)
+    seq = torch.tensor([0, 0, 0, 0, 1, 1, -1, 2, 1, -1], dtype=dtype)
+    pos = torch.tensor([-1, 0, 11, 12, -7, 2 ** 31 - 1, 3, 3, 5, -1], dtype=dtype)
+    got = cache.slots(lists, seq, pos)
+    assert got.dtype == torch.int64
+    assert got.tolist() == [-1, 20, 3, -1, -1, -1, -1, -1, 13, -1]
+    assert cache.slots(lists[:, :0], seq, pos).tolist() == [-1] * 10
+    assert cache.slots(lists[:0], seq, pos).tolist() == [-1] * 10
+    # entries of a list that name no page
+    gone = torch.tensor([[-1, 6]], dtype=torch.int32)
+    at = cache.slots(gone, torch.zeros(8, dtype=dtype), torch.arange(8, dtype=dtype))
+    assert ((at < 0) | (at >= 24)).all()
