@@ -287,9 +287,11 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     qs, os, kc, vc = q.stride(), out.stride(), k_cache.stride(), v_cache.stride()
     if not qs[2] == os[2] == kc[3] == vc[3] == 1:
         _bad(what, "the last dimension of queries, caches and outputs must be contiguous")
+    if scale is None:
+        scale = dim ** -0.5 if dim else 1.0   # (no dim: refused with the other sizes)
     try:
         desc = _ATTENTION.pack(_DTYPE[dtype], batch, tokens, heads, cache[2], dim, cache[0], cache[1], entries, causal,
-                               window, max_q, max_kv, dim ** -0.5 if scale is None else scale, qs[0], qs[1], os[0], os[1],
+                               window, max_q, max_kv, scale, qs[0], qs[1], os[0], os[1],
                                kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], page_list.stride(0))
     except (struct.error, OverflowError) as e:
         _bad(what, f"a number that its field does not hold: {e}")

@@ -57,3 +57,11 @@ def test_keys_alone_and_queries_alone_that_require_gradients():
     for q, k in ((None, k), (k, None)):
         with pytest.raises(ft.FtcnnError, match="no backward"):
             paged.qk_norm_rope(q, k)
+
+
+def test_heads_of_no_values():
+    a = arguments()
+    for name in ("q", "k_cache", "v_cache"):
+        a[name] = a[name][..., :0]
+    with pytest.raises(ft.FtcnnError, match="dim 0"):
+        attend(a)
