@@ -38,6 +38,7 @@
 #include <limits.h>
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "paged.h"
@@ -799,14 +800,26 @@ __global__ __launch_bounds__(64 * WR, DP > 128 ? 1 : 2) void attn_kernel(AttnArg
     attn_clear_unowned<T, L::THREADS>(a);
 }
 
+// The limit is a device's own, so each device that the process launches on has it raised.
+inline hipError_t raise_lds_limit(const void *kernel, int bytes, std::atomic<uint64_t> &raised) {
+    int device = 0;
+    hipError_t err = hipGetDevice(&device);
+    if (err != hipSuccess) return err;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (raised.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (err == hipSuccess) raised.fetch_or(bit, std::memory_order_relaxed);
+    return err;
+}
+
 template <typename T, int DP, int WR, int KS, bool EVEN, bool ONE>
 hipError_t attn_launch(const AttnArgs &a, unsigned blocks, hipStream_t st) {
     using L = AttnTile<T, DP, WR, KS>;
     auto kernel = attn_kernel<T, DP, WR, KS, EVEN, ONE>;
     if constexpr (L::LDS > 65536) {
-        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
-                                                           hipFuncAttributeMaxDynamicSharedMemorySize, L::LDS);
-        if (attr != hipSuccess) return attr;
+        static std::atomic<uint64_t> raised{0};   // devices whose limit is raised for this kernel
+        const hipError_t err = raise_lds_limit(reinterpret_cast<const void *>(kernel), L::LDS, raised);
+        if (err != hipSuccess) return err;
     }
     kernel<<<blocks, L::THREADS, L::LDS, st>>>(a);
     return hipGetLastError();

@@ -65,3 +65,18 @@ def test_heads_of_no_values():
         a[name] = a[name][..., :0]
     with pytest.raises(ft.FtcnnError, match="dim 0"):
         attend(a)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices in one process")
+def test_every_device_of_the_process():
+    """Kernels whose LDS is more than a launch has unasked, on one device after the other."""
+    outs = []
+    for i in range(torch.cuda.device_count()):
+        with torch.cuda.device(i):
+            torch.manual_seed(1)
+            q = torch.randn(40, 4, 256).to("cuda")
+            cache = torch.randn(2, 4, 16, 2, 256).to("cuda")
+            i32 = dict(dtype=torch.int32, device="cuda")
+            outs.append(paged.paged_attention(q, cache[0], cache[1], torch.arange(4, **i32).view(1, 4),
+                                              torch.tensor([60], **i32), torch.tensor([0, 40], **i32), 40, 60).cpu())
+    assert all(torch.equal(o, outs[0]) for o in outs) and torch.isfinite(outs[0]).all()
