@@ -42,9 +42,10 @@ _ATTENTION = struct.Struct("=13if11q")
 
 # A decode step makes these calls for every layer and token, so what they cost on the host counts: a
 # tensor's checks are one expression each, and the stream is asked for without a Stream object
-# (0.1 us; torch.cuda.current_stream() 2.7).
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_current_device = getattr(torch._C, "_cuda_getDevice", None)
+# (0.1 us; torch.cuda.current_stream() 2.7) where torch has that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _recording = torch.is_grad_enabled
 
 

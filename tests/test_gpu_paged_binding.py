@@ -1,4 +1,6 @@
 """What the Python binding of the serving operators refuses."""
+import importlib.util
+
 import pytest
 import torch
 
@@ -80,3 +82,21 @@ def test_every_device_of_the_process():
             outs.append(paged.paged_attention(q, cache[0], cache[1], torch.arange(4, **i32).view(1, 4),
                                               torch.tensor([60], **i32), torch.tensor([0, 40], **i32), 40, 60).cpu())
     assert all(torch.equal(o, outs[0]) for o in outs) and torch.isfinite(outs[0]).all()
+
+
+def test_without_torch_s_short_ways_to_stream_and_device(monkeypatch):
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    monkeypatch.delattr(torch._C, "_cuda_getDevice")
+    spec = importlib.util.spec_from_file_location("paper_2003_12203_amd.paged_again", paged.__file__)
+    again = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(again)
+    monkeypatch.undo()
+    a = arguments()
+    append(a)
+    args = (a["q"], a["k_cache"], a["v_cache"], a["page_list"], a["kv_lens"], a["q_starts"], 3, 5)
+    assert torch.equal(again.paged_attention(*args), attend(a))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = again.paged_attention(*args, stream=s)
+    s.synchronize()
+    assert torch.equal(got, attend(a))
