@@ -6,7 +6,7 @@
 // unit's rows: a team of 32 lanes (four values a lane) a row, or with fewer rows than teams several that
 // share a row's parts.
 //
-// It reads each part once: chunks over 8192 cached tokens, 64 MB of parts, 18 us; single tokens of 64 sequences 6 to 7 us
+// It reads each part once: chunks over 8192 cached tokens, 64 MB of parts, 18 to 20 us; single tokens of 64 sequences 6 to 7 us
 // (2048, 4096 or 8192 workgroups, or parts loaded before their weights are known: the same).
 #include <algorithm>
 
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a, int row
             const int from = blockIdx.y * rows_here, rows = min(cut.rows - from, rows_here);
             if (rows <= 0) continue;
             const int parts = cut.last_run - cut.first_run + 1;
-            const int share = rows >= kTeams ? 1 : (rows > 4 ? 1 : (rows > 2 ? 2 : (rows > 1 ? 4 : 8)));   // teams a row
+            const int share = rows > 4 ? 1 : (rows > 2 ? 2 : (rows > 1 ? 4 : 8));   // teams a row
             const int sub = team % share;
             for (int r0 = 0; r0 < rows; r0 += kTeams / share) {
                 const int row = from + r0 + team / share;
