@@ -488,7 +488,8 @@ typedef struct {
     int32_t causal, window;          /* window > 0 (causal only): the last window positions */
     int32_t max_q, max_kv;           /* the longest sequence's new and cached tokens; 0: not
                                         known.  They shape the launch: too small or too large
-                                        costs time, and another order of the sums         */
+                                        costs time, and changes the order of the sums and,
+                                        in bf16, which weights are rounded (see below)    */
     float scale;                     /* positive                                          */
     int64_t q_stride[2], out_stride[2];             /* token, head                        */
     int64_t k_cache_stride[3], v_cache_stride[3];   /* page, row, head                    */
@@ -505,8 +506,10 @@ typedef struct {
  * with lse (fp32 [tokens][heads], NULL: not wanted) the natural logarithm.  A row that sees
  * nothing (an empty cache, or fewer cached tokens than new ones) is 0, its lse -infinity; so are
  * rows of no sequence, before q_starts[0] and from q_starts[batch] on (padding).
- * Scores, maxima, sums and outputs are held in fp32; bf16 calls round the softmax weights,
- * relative to a maximum, to bf16 for the product with the values.
+ * Scores, maxima, sums and outputs are held in fp32.  bf16 calls of more than 16 rows a key head
+ * (max_q * heads / kv_heads) round the softmax weights, relative to a maximum, to bf16 for the
+ * product with the values, not for their sum; others keep them in fp32.  Infinities and NaN of keys
+ * and values that a row does not see do not reach it.
  * kv_lens are taken within [0, list_len * page], q_starts within [0, tokens], and a page number
  * outside [0, pages) as the nearest one inside.  Rows of q, out and the cache start on 16 bytes;
  * the cache's strides are 0 to 2^29.  out may be q.  The result does not depend on timing: calls

@@ -80,8 +80,9 @@ AttnPlan attn_plan(const ftcnn_attention_desc &d) {
     // 70 ns; a workgroup, bf16 25 ns, fp32 60 ns).  What the start and end of a unit take: a wave one tile, bf16
     // workgroups five of 64 keys (mixed chunks 117 us; three 130, one 153), fp32 two of 32.  What even runs
     // take besides, the schedule and the join: 14 us of a wave, 25 of a workgroup.  A run is not made shorter than
-    // min_run.  Whole / even: one prompt of 512 tokens 18 / 44 us, of 2048 56 / 88; chunks over 8192 cached tokens
-    // 256 / 111; 64 tokens over 500 keys 44 / 44, over 2000 169 / 114.
+    // min_run.  All of it was measured with heads of 64 and 128, and is applied to others as it is.  Whole / even: one
+    // prompt of 512 tokens 18 / 44 us, of 2048 56 / 88; chunks over 8192 cached tokens 256 / 111; 64 tokens over
+    // 500 keys 44 / 44, over 2000 169 / 114.
     p.min_run = wide ? 128 : 64;
     p.unit_cost = wide ? (bf ? 320 : 64) : 32;
     const long long rest = wide ? (bf ? 1100 : 330) : 200;

@@ -12,7 +12,10 @@
 // (lane ^ 32): softmax needs one exchange.  A lane then holds the keys 8 q + 4 half + (0..3), and
 // O^T = V^T P^T takes any order of its keys as long as both operands have the same: P stays in
 // registers, rounded to bf16 (fp32 kernels: as it is), and V is read from LDS in that order (bf16:
-// transposed on the way, four keys of 16 columns at a time).
+// transposed on the way, four keys of 16 columns at a time).  That rounding is what the bf16 matrix instructions ask
+// for; the fp32 ones would hold every bit at an eighth of their rate.  The sum takes the unrounded weights.  Outputs
+// of two prompts are within 0.0020 of float64, relative and root mean square, where exact weights leave 0.0015, the
+// outputs' own rounding.
 //
 // LDS rows are unpadded (the direct loads write 1024 consecutive bytes a wave); 16-byte units are
 // permuted within a row instead, so that what a cycle reads falls on different banks: the loads fetch
@@ -27,12 +30,14 @@
 // What bounds it, with many rows, is the matrix cores and what keeps them from being fed: the weights (an
 // exponential and its rounding for 4 dim operations) and the waits.  The scores of the next tile are multiplied
 // while this one's weights are made (one prompt's tile after the other 1157 us, so 1102), in an order written
-// by hand with scalar page addresses (1034).  Two prompts of 8192 tokens, 32 heads of 128 over eight key heads, causal, bf16:
-// 1050 us, 1050 TFLOP/s of the 1260 that a product of 8192 x 8192 matrices reaches; a rise of the matrix cores' share
-// from 45 to 55 % took the clock from 2.13 to 1.87 GHz, so the power limit is near as well.  Chunks over 8192 cached tokens
-// take twice their floor: the cut units' parts are written, read and joined (64 MB), and a workgroup's start is
-// five tiles long.  fp32, a prompt of 4096 tokens: 103 TFLOP/s of 153
-// with heads of 64, 115 with 128.
+// by hand with scalar page addresses (1034).  Two prompts of 8192 tokens, 32 heads of 128 over eight key heads,
+// causal, bf16: 1050 to 1085 us on several devices, 1010 to 1050 TFLOP/s of the 1260 that a product of 8192 x 8192
+// matrices reaches; a rise of the matrix cores' share from 45 to 55 % took the clock from 2.13 to 1.87 GHz, so the
+// power limit is near as well.  Chunks over 8192 cached tokens take twice their floor: the cut units' parts are
+// written, read and joined (64 MB), and a workgroup's start is five tiles long.  fp32, a prompt of 4096 tokens, 32
+// heads over eight key heads: 116 TFLOP/s of 153 with heads of 64, 122 with 128, 112 with 256.  Whole units are
+// dealt out once, without a look at who is done: where they are about two to a compute unit, the longest may meet on
+// one (16 heads over 16 or four: 66 TFLOP/s).
 #pragma once
 
 #include <limits.h>
@@ -610,7 +615,9 @@ template <typename T, int DP, int KS> struct AttnRows {
     }
 };
 
-// Two workgroups to a compute unit where registers hold them (fp32, heads of 128, a prompt of 4096 tokens: 597 us, one 1037).
+// Two workgroups to a compute unit where registers hold them.  fp32, heads of 128, a prompt of 4096 tokens, 32 heads over eight
+// key heads: 1118 us, one 1254; two of 8192 8.28 ms and 9.68; 1024 tokens, heads of 96: 112 and 118.  Not where the
+// longest units meet: 16 heads over 16, 1037, one 694; over eight 766 and 649.
 template <typename T, int DP, int WR, int KS, bool EVEN, bool ONE>
 __global__ __launch_bounds__(64 * WR, DP > 128 ? 1 : 2) void attn_kernel(AttnArgs a) {
     using L = AttnTile<T, DP, WR, KS>;
@@ -825,7 +832,9 @@ hipError_t attn_launch(const AttnArgs &a, unsigned blocks, hipStream_t st) {
     return hipGetLastError();
 }
 template <typename T, int DP, int WR, int KS> hipError_t attn_go(const AttnArgs &a, hipStream_t st) {
-    // page addresses in scalars (two prompts of 8192 tokens 1034 us, with an address a lane 1102)
+    // Page addresses in scalars (two prompts of 8192 tokens 1034 us, with an address a lane 1102), else one for every
+    // load of a lane, which heads of 128 have no registers for (7 to 29 spilled): pages of 24 rows, bf16, two
+    // prompts 1237 us (of 64: 1074), chunks over a cache 126 (115).
     const bool one = a.page % (AttnTile<T, DP, WR, KS>::KEYS / WR) == 0 && std::max(a.kb[1], a.vb[1]) < 1u << 24;
     const unsigned whole = (unsigned)a.tiles * a.kv_heads * a.batch;
     if (a.groups)

@@ -16,7 +16,8 @@
 //
 // Measured with the join, bf16, 32 heads of 128 over eight key heads: one token over 131072, 537 MB, 116 us
 // (105 without, 5.1 TB/s of the 5.2 that a large copy reaches); 64 single tokens over 204 MB of ragged caches 57 us (50
-// without); through LDS in workgroups that share the loads the latter took 81.  Over few keys the start is all: 76 keys
+// without); through LDS in workgroups that share the loads the latter took 81.  fp32, the same: 228 us (1.07 GB) and 86
+// (408 MB).  Over few keys the start is all: 76 keys
 // 10.5 us, in which loads wait for each other: lengths, page list, keys, and the next tile's after this one's.
 #pragma once
 

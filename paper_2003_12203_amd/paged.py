@@ -245,7 +245,8 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     pages (page_list int32 [batch][entries], kv_lens int32 [batch], the new tokens' rows among them).
     q_starts int32 [batch + 1] says whose tokens are whose (None: one of each sequence; tokens of no sequence are
     0).  max_q and max_kv, the
-    longest sequence's new and cached tokens where the caller knows them, size the launch.  scale defaults to
+    longest sequence's new and cached tokens where the caller knows them, size the launch (and, in bf16, max_q decides
+    which calls round their softmax weights).  scale defaults to
     1 / sqrt(dim).  lse (float32 [tokens][heads]) is filled when given.  workspace: uint8, 256-byte aligned;
     allocated when needed and not given."""
     what = "paged_attention"
