@@ -17,6 +17,7 @@ namespace {
 // Rows a sequence's page list can name, rows of queries, key heads of all sequences.  attn_plan's products of units
 // and keys then stay below 2^63.
 constexpr long long kMaxRows = 1LL << 30;
+constexpr long long kMaxThreads = (1LL << 32) - 1;   // of a launch
 
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -53,6 +54,8 @@ int check_rope(const char *what, int32_t dtype, int32_t tokens, int32_t heads, i
 
 }  // namespace
 
+static int attn_threads(const AttnPlan &p) { return p.rows == 16 ? 64 : 256; }   // of a workgroup
+
 AttnPlan attn_plan(const ftcnn_attention_desc &d) {
     AttnPlan p{};
     if (d.batch == 0 || d.tokens == 0) return p;   // no units
@@ -69,11 +72,15 @@ AttnPlan attn_plan(const ftcnn_attention_desc &d) {
     p.rows = wide ? 128 : 16;
     p.keys = wide ? (bf && p.dp <= 128 ? 64 : 32) : (p.dp * es <= 256 ? 32 : 16);
     const long long tile = p.rows;
-    p.tiles = (int)((rows + tile - 1) / tile);
+    const long long tiles = (rows + tile - 1) / tile;
+    // A workgroup goes on to tile t + p.tiles, so fewer do as well where all of them (without a hint of the longest
+    // sequence most have nothing to do) would pass what a launch holds.
+    const long long most = kMaxThreads / attn_threads(p) / ((long long)d.batch * d.kv_heads);
+    p.tiles = (int)std::min(tiles, std::max(1LL, most));
     // workgroups that are on the device at a time (registers and LDS)
     const bool narrow = p.dp * es <= 256;
     const long long fit = kComputeUnits * (wide ? (p.dp <= 128 ? 2 : 1) : (narrow ? 8 : 4));
-    const long long some = std::min<long long>((long long)d.batch * p.tiles, d.tokens * group / tile + d.batch);
+    const long long some = std::min<long long>((long long)d.batch * tiles, d.tokens * group / tile + d.batch);
     const long long units = some * d.kv_heads;
     const long long range = d.window > 0 ? std::min<long long>(max_kv, d.window + tile / group + 1) : max_kv;
     // Whole units or even runs: the shorter by the sizes the host knows, in the time of a key (a wave alone
@@ -268,7 +275,8 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
     if (pl.bytes && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256))
         return set_error(FTCNN_E_WORKSPACE, "%s: workspace missing or not 256-byte aligned", what);
     const long long blocks = pl.groups ? pl.groups : (long long)pl.tiles * d->kv_heads * d->batch;
-    if (blocks > 0x7fffffffLL) return set_error(FTCNN_E_SHAPE, "%s: %lld workgroups", what, blocks);
+    if (blocks * attn_threads(pl) > kMaxThreads)
+        return set_error(FTCNN_E_SHAPE, "%s: %lld workgroups", what, blocks);
     AttnArgs a{};
     a.q = q;
     a.k = k_cache;

@@ -218,7 +218,7 @@ hipError_t go(RopeArgs a, hipStream_t st) {
     a.div_chunks = fast_div((uint32_t)a.all_chunks);
     const long long ids = (long long)a.tokens * a.all_chunks;
     const long long blocks = (ids + kThreads / LPR - 1) / (kThreads / LPR);
-    if (ids >= (1LL << 31)) return hipErrorInvalidValue;
+    if (ids >= (1LL << 31) || blocks * kThreads >= (1LL << 32)) return hipErrorInvalidValue;   // past div_by, a launch
     if (past_l2) rope_kernel<T, V, LPR, UPL, true><<<(unsigned)blocks, kThreads, 0, st>>>(a);
     else rope_kernel<T, V, LPR, UPL, false><<<(unsigned)blocks, kThreads, 0, st>>>(a);
     return hipGetLastError();
@@ -285,6 +285,7 @@ hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st) {
 
 hipError_t launch_rope_table(const ftcnn_rope_scaling &sc, float *table, hipStream_t st) {
     const long long n = (long long)sc.max_pos * (sc.rot / 2);
+    if (n > (1LL << 32) - kThreads) return hipErrorInvalidValue;   // past a launch; 32 GB
     rope_table_kernel<<<(unsigned)((n + kThreads - 1) / kThreads), kThreads, 0, st>>>(
         sc, reinterpret_cast<float2 *>(table));
     return hipGetLastError();

@@ -77,3 +77,31 @@ def test_an_infinite_value_of_a_weight_below_fp32(dtype, new, length, window, ke
     got = check(q, kc, vc, lists, lens, starts, dtype, max_q=new, max_kv=length, window=window)
     assert torch.equal(first[0], got[0]) and torch.equal(first[1], got[1])
     assert torch.isposinf(got[0][:, 0, 3]).any()
+
+
+def test_many_sequences_without_hints():
+    """Row tiles for every sequence as long as all tokens together would be more workgroups than a launch holds: a
+    workgroup takes several."""
+    rng = np.random.default_rng(3)
+    tokens, sequences, heads, kv, dim, page = 1 << 17, 1024, 32, 8, 8, 16
+    torch.manual_seed(3)
+    q = torch.randn(tokens, heads, dim, device="cuda").bfloat16()
+    kc, vc = torch.randn(2, 8 * sequences, page, kv, dim, device="cuda").bfloat16()
+    lists = torch.from_numpy(rng.permutation(8 * sequences).astype(np.int32)).view(sequences, 8).cuda()
+    cut = np.sort(rng.choice(np.arange(1, tokens), sequences - 1, replace=False))
+    cut = np.concatenate(([0], cut, [tokens])).astype(np.int32)
+    lens = torch.full((sequences,), 8 * page, dtype=torch.int32, device="cuda")
+    starts, longest = torch.from_numpy(cut).cuda(), int(np.diff(cut).max())
+    tiles, blocks = (tokens * heads // kv + 127) // 128, sequences * kv
+    assert tiles * blocks * 256 > 1 << 32 and longest * heads // kv > 16
+    for kw in (dict(), dict(max_kv=8 * page)):
+        got = paged.paged_attention(q, kc, vc, lists, lens, starts, **kw)
+        want = paged.paged_attention(q, kc, vc, lists, lens, starts, longest, 8 * page)
+        assert torch.equal(got, want)
+    b = int(np.diff(cut).argmax())                                    # one sequence against the definition
+    own = slice(cut[b], cut[b + 1])
+    check(q[own], kc, vc, lists[b:b + 1].cpu().numpy(), np.array([8 * page], np.int32),
+          np.array([0, longest], np.int32), "bf16", max_q=longest, max_kv=8 * page)
+    out, _ = attend(q[own], kc, vc, lists[b:b + 1].cpu().numpy(), np.array([8 * page], np.int32),
+                    np.array([0, longest], np.int32), max_q=longest, max_kv=8 * page)
+    assert torch.equal(out, want[own])
