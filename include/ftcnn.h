@@ -490,7 +490,7 @@ typedef struct {
                                         known.  They shape the launch: too small or too large
                                         costs time, and changes the order of the sums and,
                                         in bf16, which weights are rounded (see below)    */
-    float scale;                     /* positive                                          */
+    float scale;                     /* positive, below 2.3e38                            */
     int64_t q_stride[2], out_stride[2];             /* token, head                        */
     int64_t k_cache_stride[3], v_cache_stride[3];   /* page, row, head                    */
     int64_t list_stride;

@@ -17,6 +17,7 @@ namespace {
 // Rows a sequence's page list can name, rows of queries, key heads of all sequences.  attn_plan's products of units
 // and keys then stay below 2^63.
 constexpr long long kMaxRows = 1LL << 30;
+constexpr float kLog2E = 1.44269504088896340736f;
 constexpr long long kMaxThreads = (1LL << 32) - 1;   // of a launch
 
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -133,8 +134,8 @@ int check_attention(const ftcnn_attention_desc *d) {
         return set_error(FTCNN_E_SHAPE, "%s: %d sequences of %d key heads", what, d->batch, d->kv_heads);
     if (d->window < 0 || (d->window > 0 && !d->causal))
         return set_error(FTCNN_E_ARG, "%s: window %d (0, or positive with causal)", what, d->window);
-    if (!(d->scale > 0.0f) || !std::isfinite(d->scale))
-        return set_error(FTCNN_E_ARG, "%s: scale %g (positive)", what, (double)d->scale);
+    if (!(d->scale > 0.0f) || !std::isfinite(d->scale * kLog2E))   // (the kernels take that product)
+        return set_error(FTCNN_E_ARG, "%s: scale %g (positive, below 2.3e38)", what, (double)d->scale);
     return FTCNN_OK;
 }
 
@@ -322,7 +323,7 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *d, const void *q, const vo
     a.interleave = pl.tiles > 1 && (long long)d->batch * d->kv_heads % 8 == 0;
     a.div_page = fast_div((uint32_t)d->page);
     a.div_group = fast_div((uint32_t)a.group);
-    a.scale_log2 = d->scale * 1.44269504088896340736f;
+    a.scale_log2 = d->scale * kLog2E;
     if (d->batch == 0) {
         FT_PAGED_HIP(launch_attn_clear(d->dtype, a, stream), what);
         return FTCNN_OK;

@@ -5,7 +5,7 @@ import torch
 
 import paper_2003_12203_amd as ft
 from paper_2003_12203_amd import _lib, paged
-from test_paged_abi import E_SHAPE, attention, call_attention
+from test_paged_abi import E_ARG, E_SHAPE, attention, call_attention
 
 
 @pytest.mark.parametrize("kw", [dict(batch=0, tokens=4), dict(batch=0, tokens=4, max_q=0, max_kv=0),
@@ -49,3 +49,8 @@ def test_rows_of_padding_are_nowhere(dtype):
     gone = torch.tensor([[-1, 6]], dtype=torch.int32)
     at = cache.slots(gone, torch.zeros(8, dtype=dtype), torch.arange(8, dtype=dtype))
     assert ((at < 0) | (at >= 24)).all()
+
+
+def test_a_scale_that_overflows_in_powers_of_two_is_refused():
+    assert call_attention(attention(scale=3e38)) == E_ARG
+    assert "scale" in ft.last_error()
