@@ -320,14 +320,13 @@ __device__ __forceinline__ void store4(uint16_t *p, float4 v) {
 template <typename T, int THREADS> __device__ __forceinline__ void attn_clear_unowned(const AttnArgs &a) {
     if (!a.q_starts) return;
     const int first = min(max(a.q_starts[0], 0), a.tokens), last = min(max(a.q_starts[a.batch], first), a.tokens);
-    const int count = first + a.tokens - last, quads = a.dim / 4, heads = a.kv_heads * a.group;
+    const int count = first + a.tokens - last, heads = a.kv_heads * a.group, col = 4 * (threadIdx.x % 64);   // dim <= 256
     for (int i = blockIdx.x; i < count; i += gridDim.x) {
         const long long token = i < first ? i : last + (i - first);
         T *row = static_cast<T *>(a.o) + token * a.os[0];
-        for (int x = threadIdx.x; x < heads * quads; x += THREADS) {
-            const int head = x / quads;
-            store4(row + head * a.os[1] + 4 * (x - head * quads), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
-        }
+        if (col < a.dim)
+            for (int head = threadIdx.x / 64; head < heads; head += THREADS / 64)
+                store4(row + head * a.os[1] + col, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
         if (a.lse)
             for (int h = threadIdx.x; h < heads; h += THREADS) a.lse[token * heads + h] = -INFINITY;
     }
