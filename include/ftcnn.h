@@ -523,6 +523,94 @@ int ftcnn_paged_attention(const ftcnn_attention_desc *desc, const void *q, const
  * where it needs none (NULL will do), and on a bad descriptor. */
 size_t ftcnn_paged_attention_workspace_bytes(const ftcnn_attention_desc *desc);
 
+/* ---- what differs from request to request ----------------------------------
+ * Requests that one layer serves together may bring adapters of their own beside its projections, and
+ * keep their caches within budgets of their own.  Conventions are those of the serving operators above:
+ * strides in elements, innermost dimensions contiguous, fp32 arithmetic, results rounded once, and index
+ * arrays on the device, brought into range by the kernels. */
+
+typedef struct {
+    int32_t dtype, tokens;
+    int32_t ch, m;                   /* of the projection; multiples of 16 bytes          */
+    int32_t adapters, rank;          /* rank: a multiple of 16 bytes, at most 128         */
+    int64_t x_stride, y_stride, out_stride;      /* token                                 */
+    int64_t a_stride[2], b_stride[2];            /* adapter, row                          */
+} ftcnn_low_rank_desc;
+
+/* out_t = y_t + scales[a] B_a (A_a x_t) with a = ids[t]: x [tokens][ch], the output y [tokens][m] of the
+ * projection that all tokens share, A [adapters][rank][ch], B [adapters][m][rank].  ids [tokens] may come in
+ * any order; a token whose id is not in [0, adapters) (none: -1) keeps y as it is.  scales (fp32
+ * [adapters], NULL: 1).  ranks [adapters] (NULL: rank): adapter a has the first ranks[a] rows of A_a and
+ * columns of B_a, taken within [0, rank]; what lies past them is not used.  A_a x_t is held in fp32; bf16:
+ * for the second product as the sum of two bf16 values, within 2^-16 of it.  Infinities and NaN of a token
+ * or adapter reach only the tokens that have them.  An infinity in B comes out as itself or as NaN.
+ * out may be y (with its strides); outputs that overlap inputs otherwise are undefined.  Rows start on 16
+ * bytes.  The workspace holds the products A x.  The result does not depend on timing.  Two launches. */
+int ftcnn_low_rank_add(const ftcnn_low_rank_desc *desc, const void *y, const void *x, const void *a, const void *b,
+                       const int32_t *ids, const float *scales, const int32_t *ranks, void *out, void *workspace,
+                       hipStream_t stream);
+
+/* Bytes of 256-byte-aligned workspace of the call; 0 where it needs none, and on a bad descriptor. */
+size_t ftcnn_low_rank_workspace_bytes(const ftcnn_low_rank_desc *desc);
+
+typedef struct {
+    int32_t dtype, batch, tokens;    /* as in ftcnn_attention_desc, to scale              */
+    int32_t heads, kv_heads, dim;
+    int32_t pages, page, list_len;
+    int32_t causal, window;
+    int32_t max_q, max_kv;           /* shape the launch, as there                        */
+    float scale;
+    int64_t q_stride[2];             /* token, head                                       */
+    int64_t k_cache_stride[3];       /* page, row, head                                   */
+    int64_t mass_stride;             /* sequence; at least list_len * page                */
+    int64_t list_stride;
+} ftcnn_mass_desc;
+
+/* The softmax weight that every cached key got from the new tokens, of all heads:
+ *   mass[b][j] += sum over the rows i of sequence b that see position j of exp(scale q_i . k_j - lse_i)
+ * for j < kv_lens[b], with the queries, cache, lists, lengths and masks of the ftcnn_paged_attention call
+ * before, and the lse (fp32 [tokens][heads]) that it gave.  mass is fp32 [batch][list_len * page]; what lies
+ * past kv_lens[b] is left as it was.  Infinities and NaN of keys and rows reach only each other.  Indices are
+ * taken as there; rows of q and the cache start on 16 bytes.  The result does not depend on timing.  One
+ * launch, or two where workgroups share a key's rows: then the workspace holds the parts. */
+int ftcnn_attention_mass(const ftcnn_mass_desc *desc, const void *q, const void *k_cache, const int32_t *page_list,
+                         const int32_t *kv_lens, const int32_t *q_starts, const float *lse, float *mass, void *workspace,
+                         hipStream_t stream);
+
+/* Bytes of 256-byte-aligned workspace of the call; 0 where it needs none, and on a bad descriptor. */
+size_t ftcnn_attention_mass_workspace_bytes(const ftcnn_mass_desc *desc);
+
+typedef struct {
+    int32_t dtype, batch;
+    int32_t kv_heads, dim;
+    int32_t pages, page, list_len;
+    int32_t first;                   /* rows at positions below it are kept               */
+    int32_t max_kv;                  /* the longest sequence's rows (0: not known): shapes the launch */
+    int32_t reserved;
+    int64_t k_cache_stride[3], v_cache_stride[3];   /* page, row, head                    */
+    int64_t list_stride;
+    int64_t mass_stride, position_stride, mass_out_stride, position_out_stride;   /* sequence */
+} ftcnn_evict_desc;
+
+/* Takes rows out of the sequences' caches: of the n = kv_lens[b] rows of sequence b, k = min(keep[b], n) stay,
+ * and the length becomes lens_out[b] = k.  Those stay that come first by: kept for its position or not, then
+ * larger mass[b][j] (NaN below all), then lower place j.  A row is kept for its position where
+ * positions[b][j] < first or positions[b][j] >= since[b] (since NULL: no such); positions NULL: a row's place is
+ * its position.  The i-th place below k whose row goes takes the keys and values of all heads of the i-th row
+ * that stays from place k on, so rows do not stay in the order of their positions: attention over them is the
+ * same in any order, but not with a window, which goes by places.  mass_out and positions_out
+ * [batch][list_len * page] move with the rows; from place k on they are 0 and -1.  They may be mass and
+ * positions, and lens_out may be kv_lens.  Cache rows from place k on keep what they held.
+ * A page that is listed twice, in one sequence or two, holds undefined values after it.  keep and kv_lens are
+ * taken as at least 0, kv_lens as at most list_len * page, page numbers as in ftcnn_paged_attention.  Rows of the
+ * cache start on 16 bytes; its strides are 0 to 2^29.  Two launches. */
+int ftcnn_evict(const ftcnn_evict_desc *desc, void *k_cache, void *v_cache, const int32_t *page_list, const int32_t *kv_lens,
+                const int32_t *keep, const float *mass, const int32_t *positions, const int32_t *since, int32_t *lens_out,
+                float *mass_out, int32_t *positions_out, void *workspace, hipStream_t stream);
+
+/* Bytes of 256-byte-aligned workspace of the call; 0 on a bad descriptor. */
+size_t ftcnn_evict_workspace_bytes(const ftcnn_evict_desc *desc);
+
 #ifdef __cplusplus
 }
 #endif

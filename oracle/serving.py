@@ -118,3 +118,89 @@ def attention(q, k_cache, v_cache, page_list, kv_lens, q_starts=None, scale=None
                     bo[t, g] = rel * size + U_OUT[dtype] * np.abs(out[t, g]) * (1 + rel)
                     bl[t, g] = ds + (len(s) + 32) * U32 + 4 * U32 * abs(lse[t, g])
     return out, lse, bo, bl
+
+
+def low_rank_add(y, x, a, b, ids, scales=None, ranks=None, dtype="f32"):
+    """-> (out, bound): y[t] + scales[i] b[i] (a[i] x[t]) of the first ranks[i] rows of a[i], i = ids[t].
+
+    A value of a x is within (ch + 8) units of its sum of magnitudes (ch terms in any order, the scale's product among
+    the rest); as two bf16 values within 2^-16 of itself; the sum over the rank within (rank + 4) units of its own."""
+    y, x, a, b = (np.asarray(t, np.float64) for t in (y, x, a, b))
+    out, bound = y.copy(), np.zeros(y.shape)
+    for t, i in enumerate(ids):
+        if not 0 <= i < a.shape[0]:
+            continue
+        r = a.shape[1] if ranks is None else min(max(int(ranks[i]), 0), a.shape[1])
+        s = 1.0 if scales is None else float(scales[i])
+        low, size = s * (a[i, :r] @ x[t]), abs(s) * (np.abs(a[i, :r]) @ np.abs(x[t]))
+        off = (x.shape[1] + 8) * U32 * size + (2.0 ** -16 * np.abs(low) if dtype == "bf16" else 0.0)
+        add, mag = b[i, :, :r] @ low, np.abs(b[i, :, :r]) @ np.abs(low)
+        err = np.abs(b[i, :, :r]) @ off
+        err = err + (r + 4) * U32 * (mag + err)
+        out[t] = y[t] + add
+        bound[t] = err + (U32 + U_OUT[dtype]) * (np.abs(out[t]) + err)
+    return out, bound
+
+
+def attention_mass(mass, q, k_cache, page_list, kv_lens, lse, q_starts=None, scale=None, causal=True, window=0):
+    """-> (mass, bound): to mass[b][j] the weights exp(s - lse) of the rows and heads that see position j."""
+    q, lse = np.asarray(q, np.float64), np.asarray(lse, np.float64)
+    heads, dim = q.shape[1:]
+    page, kv_heads = k_cache.shape[1:3]
+    group = heads // kv_heads
+    scale = 1.0 / np.sqrt(dim) if scale is None else scale
+    out = np.array(mass, np.float64)
+    bound = np.zeros(out.shape)
+    for b, n in enumerate(kv_lens):
+        n = int(n)
+        lo, hi = (b, b + 1) if q_starts is None else (int(q_starts[b]), int(q_starts[b + 1]))
+        rows = [(int(page_list[b][j // page]), j % page) for j in range(n)]
+        add, err, terms = np.zeros(n), np.zeros(n), np.zeros(n)
+        for h in range(kv_heads):
+            K = np.array([k_cache[r][h] for r in rows], np.float64).reshape(n, dim)
+            for t in range(lo, hi):
+                p = n - (hi - lo) + (t - lo)
+                first = max(0, p - window + 1) if window else 0
+                last = min(p, n - 1) if causal else n - 1
+                if last < first:
+                    continue
+                seen = slice(first, last + 1)
+                for g in range(h * group, (h + 1) * group):
+                    s = K[seen] @ q[t, g] * scale
+                    w = np.exp(s - lse[t, g])
+                    # a score's sum and products; the argument's two roundings and the power's
+                    ds = (dim + 8) * U32 * scale * (np.abs(K[seen]) @ np.abs(q[t, g])) + 8 * U32 * np.abs(s)
+                    ds = ds + 4 * U32 * (np.abs(lse[t, g]) + np.abs(s - lse[t, g]) + 1)
+                    add[seen] += w
+                    err[seen] += w * np.expm1(ds) + 2.0 ** -120
+                    terms[seen] += 1
+        out[b, :n] += add
+        bound[b, :n] = err + (terms + 8) * U32 * (add + err) + 2 * U32 * np.abs(out[b, :n])
+    return out, bound
+
+
+def evict(k_cache, v_cache, page_list, kv_lens, keep, mass, positions=None, first=0, since=None):
+    """-> (k_cache, v_cache, lens, mass, positions), exactly."""
+    kc, vc = k_cache.copy(), v_cache.copy()
+    page = kc.shape[1]
+    lens, out, pos = [], np.zeros(mass.shape, np.float32), np.full(mass.shape, -1, np.int32)
+    for b, n in enumerate(kv_lens):
+        n = int(n)
+        k = min(max(int(keep[b]), 0), n)
+        p = [int(x) for x in positions[b][:n]] if positions is not None else list(range(n))
+        late = int(since[b]) if since is not None else 1 << 40
+
+        def order(j):
+            w = float(mass[b][j])
+            return (not (p[j] < first or p[j] >= late), w != w, 0.0 if w != w else -w, j)
+
+        stay = set(sorted(range(n), key=order)[:k])
+        holes, movers = [j for j in range(k) if j not in stay], [j for j in range(k, n) if j in stay]
+        source = list(range(k))
+        for to, at in zip(holes, movers):
+            source[to] = at
+            rt, ra = (int(page_list[b][to // page]), to % page), (int(page_list[b][at // page]), at % page)
+            kc[rt], vc[rt] = kc[ra], vc[ra]
+        out[b, :k], pos[b, :k] = mass[b][source], [p[j] for j in source]
+        lens.append(k)
+    return kc, vc, np.array(lens, np.int32), out, pos

@@ -79,13 +79,36 @@ class AttentionDesc(C.Structure):
         ("k_cache_stride", C.c_int64 * 3), ("v_cache_stride", C.c_int64 * 3), ("list_stride", C.c_int64)]
 
 
+class LowRankDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "ch", "m", "adapters", "rank")] + [
+        (n, C.c_int64) for n in ("x_stride", "y_stride", "out_stride")] + [
+        ("a_stride", C.c_int64 * 2), ("b_stride", C.c_int64 * 2)]
+
+
+class MassDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "batch", "tokens", "heads", "kv_heads", "dim", "pages", "page",
+                                         "list_len", "causal", "window", "max_q", "max_kv")] + [
+        ("scale", C.c_float), ("q_stride", C.c_int64 * 2), ("k_cache_stride", C.c_int64 * 3),
+        ("mass_stride", C.c_int64), ("list_stride", C.c_int64)]
+
+
+class EvictDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "batch", "kv_heads", "dim", "pages", "page", "list_len", "first",
+                                         "max_kv", "reserved")] + [
+        ("k_cache_stride", C.c_int64 * 3), ("v_cache_stride", C.c_int64 * 3)] + [
+        (n, C.c_int64) for n in ("list_stride", "mass_stride", "position_stride", "mass_out_stride",
+                                 "position_out_stride")]
+
+
 EXPORTS = ("ftcnn_out_shape", "ftcnn_workspace_bytes", "ftcnn_report_bytes", "ftcnn_last_error",
            "ftcnn_encode", "ftcnn_conv_fwd", "ftcnn_checksum_conv", "ftcnn_verify", "ftcnn_correct",
            "ftcnn_verify_correct", "ftcnn_conv_fwd_ws", "ftcnn_conv_fwd_sums", "ftcnn_verify_correct_sums", "ftcnn_protected_conv",
            "ftcnn_inject", "ftcnn_set_kernel_events", "ftcnn_conv_fwd_bias", "ftcnn_check_weights",
            "ftcnn_relu_pool", "ftcnn_relu_pool_encode", "ftcnn_conv_fwd_sums_given", "ftcnn_conv_tile",
            "ftcnn_protected_conv_noalloc", "ftcnn_conv_stream_k", "ftcnn_rope_table", "ftcnn_qk_norm_rope",
-           "ftcnn_kv_append", "ftcnn_paged_attention", "ftcnn_paged_attention_workspace_bytes")
+           "ftcnn_kv_append", "ftcnn_paged_attention", "ftcnn_paged_attention_workspace_bytes",
+           "ftcnn_low_rank_add", "ftcnn_low_rank_workspace_bytes", "ftcnn_attention_mass",
+           "ftcnn_attention_mass_workspace_bytes", "ftcnn_evict", "ftcnn_evict_workspace_bytes")
 
 _lib = None
 
@@ -164,5 +187,14 @@ def load(path: str = LIB_PATH):
     L.ftcnn_paged_attention.restype = C.c_int
     L.ftcnn_paged_attention_workspace_bytes.argtypes = [C.c_char_p]
     L.ftcnn_paged_attention_workspace_bytes.restype = C.c_size_t
+    L.ftcnn_low_rank_add.argtypes = [C.c_char_p] + [_dp] * 10
+    L.ftcnn_low_rank_add.restype = C.c_int
+    L.ftcnn_attention_mass.argtypes = [C.c_char_p] + [_dp] * 9
+    L.ftcnn_attention_mass.restype = C.c_int
+    L.ftcnn_evict.argtypes = [C.c_char_p] + [_dp] * 13
+    L.ftcnn_evict.restype = C.c_int
+    for name in ("low_rank", "attention_mass", "evict"):
+        f = getattr(L, f"ftcnn_{name}_workspace_bytes")
+        f.argtypes, f.restype = [C.c_char_p], C.c_size_t
     _lib = L
     return L

@@ -1,0 +1,25 @@
+// Internal definitions of the eviction from a paged cache.  Not part of the C ABI.
+#pragma once
+
+#include "paged.h"
+
+namespace ftcnn {
+
+struct EvictArgs {
+    void *k, *v;
+    unsigned kb[3], vb[3];        // bytes: page, row, head
+    const int32_t *page_list, *kv_lens, *keep, *positions, *since;
+    const float *mass;
+    int32_t *lens_out, *positions_out;
+    float *mass_out;
+    long long list_stride, ms, ps, mos, pos;   // elements between sequences: mass, positions, and those written
+    int batch, kv_heads, pages, page, capacity, first;
+    int units;                    // 16-byte units of a row of a head
+    int32_t *counts, *from, *to;  // workspace: moves of each sequence, [batch] and [batch][half]
+    long long half;
+    int shares;                   // workgroups that share a sequence's moves
+    FastDiv div_page;
+};
+hipError_t launch_evict(const EvictArgs &a, hipStream_t st);
+
+}  // namespace ftcnn

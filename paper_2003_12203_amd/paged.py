@@ -1,5 +1,6 @@
 """The operators of a serving attention layer: norms and rotation of queries and keys, a paged cache of
-keys and values, and the attention of new tokens over it.
+keys and values, the attention of new tokens over it, and what keeps the cache within a budget: the weight that
+each key gets, summed, and the eviction of the rows that got the least.
 
 They stand between the projections of a transformer layer, which are layers of 1x1 maps with the
 tokens as the batch (``Layer(tokens, ch, 1, 1, m, 1, 1)``: checksum-protected matrix products).  The
@@ -17,7 +18,9 @@ backward passes: where gradients are recorded (not under ``torch.no_grad()``), a
     cache = paged.PagedCache(pages, page, kv_heads, dim, "bf16")
     q, _ = paged.qk_norm_rope(q, None, positions, table, q_weight)
     paged.kv_append(k, v, cache.k, cache.v, slots, positions, table, k_weight)
-    out = paged.paged_attention(q, cache.k, cache.v, page_list, kv_lens, q_starts, max_q, max_kv)
+    out = paged.paged_attention(q, cache.k, cache.v, page_list, kv_lens, q_starts, max_q, max_kv, lse=lse)
+    paged.attention_mass(mass, q, cache.k, page_list, kv_lens, lse, q_starts, max_q, max_kv)
+    kv_lens, mass, positions = paged.evict(cache.k, cache.v, page_list, kv_lens, keep, mass, positions, since=since)
 """
 from __future__ import annotations
 
@@ -35,10 +38,12 @@ _F32, _BF16, _I32, _I64, _U8 = torch.float32, torch.bfloat16, torch.int32, torch
 _DTYPE = {_F32: F32, _BF16: BF16}
 _CONTIGUOUS = torch.contiguous_format
 
-# the descriptors in the layout of _lib.RopeDesc, AppendDesc and AttentionDesc
+# the descriptors in the layout of _lib.RopeDesc, AppendDesc, AttentionDesc, MassDesc and EvictDesc
 _ROPE = struct.Struct("=9if8q")
 _APPEND = struct.Struct("=10ifi10q")
 _ATTENTION = struct.Struct("=13if11q")
+_MASS = struct.Struct("=13if7q")
+_EVICT = struct.Struct("=10i11q")
 
 # A decode step makes these calls for every layer and token, so what they cost on the host counts: a
 # tensor's checks are one expression each, and the stream is asked for without a Stream object
@@ -80,6 +85,38 @@ def _no_backward(what: str):
 
 def _fail(what: str, rc: int):
     _check(rc, "ftcnn_" + what)
+
+
+def _room(what: str, need: int, workspace: Optional[torch.Tensor], dev: int) -> Optional[torch.Tensor]:
+    """The workspace of a call on device dev: none where it needs none, else the given one or a new one."""
+    if not need:
+        return None
+    if workspace is None:
+        return torch.empty(need, dtype=_U8, device=f"cuda:{dev}")
+    if not (workspace.dtype is _U8 and workspace.numel() >= need and workspace.is_contiguous() and
+            workspace.get_device() == dev):
+        _bad(what, f"the workspace must be {need} contiguous bytes on device {dev}, not {_is(workspace)}")
+    return workspace
+
+
+def _lists(what, page_list, kv_lens, dev) -> Tuple[int, int]:
+    """(batch, entries) of a call's page lists."""
+    lists = page_list.shape
+    if not (page_list.dtype is _I32 and len(lists) == 2 and (page_list.stride(1) == 1 or lists[1] < 2) and
+            page_list.get_device() == dev):
+        _bad(what, f"page_list must be int32 [batch][entries], entries contiguous, on device {dev}, not "
+                   f"{_is(page_list)}")
+    if not (kv_lens.dtype is _I32 and kv_lens.shape == (lists[0],) and kv_lens.is_contiguous() and
+            kv_lens.get_device() == dev):
+        _bad(what, f"kv_lens must be a contiguous int32 [{lists[0]}] on device {dev}, not {_is(kv_lens)}")
+    return lists[0], lists[1]
+
+
+def _places(what, name, t, dtype, batch, capacity, dev):
+    """Checks a tensor of a value a place, [batch][places], of which a call takes the first `capacity`."""
+    if not (t.dtype is dtype and len(t.shape) == 2 and t.shape[0] == batch and t.shape[1] >= capacity and
+            (t.stride(1) == 1 or t.shape[1] < 2) and t.get_device() == dev):
+        _bad(what, f"{name} must be {dtype} [{batch}][{capacity} or more], places contiguous, on device {dev}, not {_is(t)}")
 
 
 def rope_table(max_pos: int, rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
@@ -313,6 +350,118 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     if rc:
         _fail(what, rc)
     return out
+
+
+def attention_mass(mass: torch.Tensor, q: torch.Tensor, k_cache: torch.Tensor, page_list: torch.Tensor,
+                   kv_lens: torch.Tensor, lse: torch.Tensor, q_starts: Optional[torch.Tensor] = None, max_q: int = 0,
+                   max_kv: int = 0, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """ftcnn_attention_mass: to mass [batch][places] (float32, a place for each row that a page list can name) the softmax
+    weight that each cached key got from the new tokens q, of all heads.  The other arguments are those of the
+    paged_attention call before, and the lse that it filled.  Returns mass."""
+    what = "attention_mass"
+    dtype, shape, dev = q.dtype, q.shape, q.get_device()
+    if dtype not in _DTYPE or len(shape) != 3 or dev < 0:
+        _bad(what, f"queries are float32 or bfloat16 [tokens][heads][dim] on a device, not {_is(q)}")
+    if stream is not None or dev != _current_device():
+        with _On(q.device, stream):
+            return attention_mass(mass, q, k_cache, page_list, kv_lens, lse, q_starts, max_q, max_kv, scale, causal,
+                                  window, workspace)
+    if _recording() and (q.requires_grad or k_cache.requires_grad or lse.requires_grad or mass.requires_grad):
+        _no_backward(what)
+    tokens, heads, dim = shape
+    cache = k_cache.shape
+    if not (k_cache.dtype is dtype and len(cache) == 4 and cache[3] == dim and k_cache.get_device() == dev):
+        _bad(what, f"k_cache must be {dtype} [pages][page][kv_heads][{dim}] on device {dev}, not {_is(k_cache)}")
+    batch, entries = _lists(what, page_list, kv_lens, dev)
+    if q_starts is not None and not (q_starts.dtype is _I32 and q_starts.shape == (batch + 1,) and
+                                     q_starts.is_contiguous() and q_starts.get_device() == dev):
+        _bad(what, f"q_starts must be a contiguous int32 [{batch + 1}] on device {dev}, not {_is(q_starts)}")
+    if q_starts is None:
+        max_q = 1
+    if not (lse.dtype is _F32 and lse.shape == (tokens, heads) and lse.is_contiguous() and lse.get_device() == dev):
+        _bad(what, f"lse must be a contiguous float32 [{tokens}][{heads}] on device {dev}, not {_is(lse)}")
+    _places(what, "mass", mass, _F32, batch, entries * cache[1], dev)
+    qs, kc = q.stride(), k_cache.stride()
+    if not qs[2] == kc[3] == 1:
+        _bad(what, "the last dimension of queries and cache must be contiguous")
+    if scale is None:
+        scale = dim ** -0.5 if dim else 1.0   # (no dim: refused with the other sizes)
+    try:
+        desc = _MASS.pack(_DTYPE[dtype], batch, tokens, heads, cache[2], dim, cache[0], cache[1], entries, causal, window,
+                          max_q, max_kv, scale, qs[0], qs[1], kc[0], kc[1], kc[2], mass.stride(0), page_list.stride(0))
+    except (struct.error, OverflowError) as e:
+        _bad(what, f"a number that its field does not hold: {e}")
+    L = _lib.load()
+    room = _room(what, L.ftcnn_attention_mass_workspace_bytes(desc), workspace, dev)
+    rc = L.ftcnn_attention_mass(desc, q.data_ptr(), k_cache.data_ptr(), page_list.data_ptr(), kv_lens.data_ptr(),
+                                None if q_starts is None else q_starts.data_ptr(), lse.data_ptr(), mass.data_ptr(),
+                                None if room is None else room.data_ptr(), _raw_stream(dev))
+    if rc:
+        _fail(what, rc)
+    return mass
+
+
+def evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_list: torch.Tensor, kv_lens: torch.Tensor,
+          keep: torch.Tensor, mass: torch.Tensor, positions: Optional[torch.Tensor] = None, first: int = 0,
+          since: Optional[torch.Tensor] = None, max_kv: int = 0, lens_out: Optional[torch.Tensor] = None,
+          mass_out: Optional[torch.Tensor] = None, positions_out: Optional[torch.Tensor] = None,
+          workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """ftcnn_evict: of each sequence's kv_lens rows keep (int32 [batch]) stay, those at positions below `first` or
+    from since (int32 [batch]) on and then those of the largest mass (float32 [batch][places]).  Rows that stay move into
+    places that become free, so the caches change, and a row's position is no longer its place: positions (int32
+    [batch][places]; None: still the places) say which it is.  Returns the new (lens, mass, positions), allocated
+    unless given (in place: lens_out=kv_lens, mass_out=mass, positions_out=positions).  No page may be listed twice.
+    workspace: uint8, 256-byte aligned; allocated when not given."""
+    what = "evict"
+    dtype, cache, dev = k_cache.dtype, k_cache.shape, k_cache.get_device()
+    if dtype not in _DTYPE or len(cache) != 4 or dev < 0:
+        _bad(what, f"k_cache is float32 or bfloat16 [pages][page][kv_heads][dim] on a device, not {_is(k_cache)}")
+    if stream is not None or dev != _current_device():
+        with _On(k_cache.device, stream):
+            return evict(k_cache, v_cache, page_list, kv_lens, keep, mass, positions, first, since, max_kv, lens_out,
+                         mass_out, positions_out, workspace)
+    if _recording() and (k_cache.requires_grad or v_cache.requires_grad or mass.requires_grad or
+                         (mass_out is not None and mass_out.requires_grad)):
+        _no_backward(what)
+    if not (v_cache.dtype is dtype and v_cache.shape == cache and v_cache.get_device() == dev):
+        _bad(what, f"v_cache must be like k_cache, {dtype} {tuple(cache)} on device {dev}, not {_is(v_cache)}")
+    batch, entries = _lists(what, page_list, kv_lens, dev)
+    capacity = entries * cache[1]
+    for name, t in (("keep", keep), ("since", since), ("lens_out", lens_out)):
+        if t is not None and not (t.dtype is _I32 and t.shape == (batch,) and t.is_contiguous() and t.get_device() == dev):
+            _bad(what, f"{name} must be a contiguous int32 [{batch}] on device {dev}, not {_is(t)}")
+    _places(what, "mass", mass, _F32, batch, capacity, dev)
+    if positions is not None:
+        _places(what, "positions", positions, _I32, batch, capacity, dev)
+    if lens_out is None:
+        lens_out = torch.empty_like(kv_lens)
+    if mass_out is None:
+        mass_out = torch.empty((batch, capacity), dtype=_F32, device=k_cache.device)
+    else:
+        _places(what, "mass_out", mass_out, _F32, batch, capacity, dev)
+    if positions_out is None:
+        positions_out = torch.empty((batch, capacity), dtype=_I32, device=k_cache.device)
+    else:
+        _places(what, "positions_out", positions_out, _I32, batch, capacity, dev)
+    kc, vc = k_cache.stride(), v_cache.stride()
+    if not kc[3] == vc[3] == 1:
+        _bad(what, "the last dimension of the caches must be contiguous")
+    try:
+        desc = _EVICT.pack(_DTYPE[dtype], batch, cache[2], cache[3], cache[0], cache[1], entries, first, max_kv, 0,
+                           kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], page_list.stride(0), mass.stride(0),
+                           0 if positions is None else positions.stride(0), mass_out.stride(0), positions_out.stride(0))
+    except (struct.error, OverflowError) as e:
+        _bad(what, f"a number that its field does not hold: {e}")
+    L = _lib.load()
+    room = _room(what, L.ftcnn_evict_workspace_bytes(desc), workspace, dev)
+    rc = L.ftcnn_evict(desc, k_cache.data_ptr(), v_cache.data_ptr(), page_list.data_ptr(), kv_lens.data_ptr(),
+                       keep.data_ptr(), mass.data_ptr(), None if positions is None else positions.data_ptr(),
+                       None if since is None else since.data_ptr(), lens_out.data_ptr(), mass_out.data_ptr(),
+                       positions_out.data_ptr(), None if room is None else room.data_ptr(), _raw_stream(dev))
+    if rc:
+        _fail(what, rc)
+    return lens_out, mass_out, positions_out
 
 
 class PagedCache:

@@ -1,0 +1,199 @@
+"""Low-rank adapters of many requests (ftcnn_low_rank_add) against their definition in float64."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2003_12203_amd as ft
+from oracle import serving as sv
+from paper_2003_12203_amd import adapters
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def make(seed, tokens, ch, m, count, rank, dtype, ids=None, none=0.2):
+    g = torch.Generator().manual_seed(seed)
+
+    def normal(*shape, scale=1.0):
+        return (torch.randn(shape, generator=g) * scale).to("cuda", DT[dtype])
+
+    if ids is None:
+        ids = torch.randint(0, count, (tokens,), generator=g)
+        ids = torch.where(torch.rand(tokens, generator=g) < none, -1, ids)
+    return dict(y=normal(tokens, m), x=normal(tokens, ch), a=normal(count, rank, ch, scale=ch ** -0.5),
+                b=normal(count, m, rank, scale=rank ** -0.5), ids=torch.as_tensor(ids, dtype=torch.int32).cuda(),
+                scales=(0.25 + torch.rand(count, generator=g)).cuda())
+
+
+def check(s, got, dtype, ranks=None):
+    want, bound = sv.low_rank_add(f64(s["y"]), f64(s["x"]), f64(s["a"]), f64(s["b"]), s["ids"].tolist(),
+                                  None if s["scales"] is None else f64(s["scales"]),
+                                  None if ranks is None else ranks.tolist(), dtype)
+    off = np.abs(f64(got) - want)
+    assert np.all(off <= bound), f"{np.max(off - bound)} over, {np.argwhere(off > bound)[:5]}"
+    count = s["a"].shape[0]
+    none = ((s["ids"] < 0) | (s["ids"] >= count))
+    assert torch.equal(got[none], s["y"][none])
+
+
+SIZES = [  # tokens, ch, m, adapters, rank: each tile size, ranks of each compiled width, tails everywhere
+    (1, 64, 64, 1, 8), (1, 4096, 6144, 8, 16), (2, 8, 8, 3, 8), (15, 40, 72, 4, 16), (16, 4096, 264, 16, 32),
+    (17, 1000, 1288, 5, 24), (64, 512, 512, 48, 40), (65, 264, 136, 2, 64), (130, 128, 1032, 7, 128), (256, 96, 64, 3, 72),
+    (257, 264, 328, 9, 16), (300, 72, 2056, 4, 64), (320, 2048, 40, 1, 8), (511, 136, 200, 70, 24), (290, 512, 104, 3, 128),
+    (600, 88, 96, 2, 104)]
+
+
+@pytest.mark.parametrize("tokens,ch,m,count,rank", SIZES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_against_float64(tokens, ch, m, count, rank, dtype):
+    s = make(tokens + rank, tokens, ch, m, count, rank, dtype)
+    check(s, adapters.low_rank_add(**s), dtype)
+
+
+@pytest.mark.parametrize("rank,ch,m", [(4, 4, 4), (12, 20, 36), (20, 1004, 516), (100, 12, 260)])
+def test_fp32_sizes_of_four(rank, ch, m):
+    s = make(rank, 33, ch, m, 3, rank, "f32")
+    check(s, adapters.low_rank_add(**s), "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [40, 400])
+def test_ranks_and_what_lies_past_them(tokens, dtype):
+    """Ranks of every kind, NaN past them, and adapters that no token has."""
+    s = make(3, tokens, 200, 144, 9, 24, dtype)
+    ranks = torch.tensor([0, 1, 7, 8, 9, 24, 100, -3, 17], dtype=torch.int32)
+    s["ids"][s["ids"] == 5] = 4
+    clean = {k: v.clone() for k, v in s.items()}
+    for i, r in enumerate(ranks.clamp(0, 24).tolist()):
+        s["a"][i, r:] = float("nan")
+        s["b"][i, :, r:] = float("inf")
+        clean["a"][i, r:] = clean["b"][i, :, r:] = 0.0
+    s["a"][5], s["b"][5] = float("nan"), float("nan")
+    got = adapters.low_rank_add(**s, ranks=ranks.cuda())
+    check(clean, got, dtype, ranks)
+
+
+@pytest.mark.parametrize("tokens", [20, 300])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_values_that_are_not_finite_reach_only_their_token(tokens, dtype):
+    s = make(4, tokens, 96, 80, 3, 16, dtype)
+    clean = adapters.low_rank_add(**s)
+    s["x"][7, 5], s["x"][11, 0] = float("nan"), float("inf")
+    s["ids"][7] = s["ids"][11] = 1
+    s["y"][13, 2] = float("inf")
+    got = adapters.low_rank_add(**s)
+    others = torch.ones(tokens, dtype=torch.bool)
+    others[[7, 11, 13]] = False
+    assert torch.equal(got[others], clean[others])
+    assert got[7].isnan().all() and not got[11].isfinite().any() and got[13, 2] == float("inf")
+    assert got[13, 3:].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ids_out_of_range_are_no_adapter(dtype):
+    ids = [0, -1, 3, 2, 2 ** 31 - 1, -2 ** 31, 1, 4]
+    s = make(5, 8, 64, 64, 3, 16, dtype, ids)
+    check(s, adapters.low_rank_add(**s), dtype)
+    s["ids"].fill_(-1)
+    assert torch.equal(adapters.low_rank_add(**s), s["y"])
+
+
+@pytest.mark.parametrize("tokens", [9, 270])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layouts(tokens, dtype):
+    """Slices of packed rows, weights inside larger ones, in place, an output with rows of its own."""
+    s = make(6, tokens, 128, 96, 4, 16, dtype)
+    want = adapters.low_rank_add(**s)
+    wide = {k: torch.full((tokens, 400), 7.0, dtype=DT[dtype], device="cuda") for k in ("x", "y", "out")}
+    x, y, out = wide["x"][:, 8:136], wide["y"][:, 64:160], wide["out"][:, 200:296]
+    x.copy_(s["x"]), y.copy_(s["y"])
+    a = torch.zeros(8, 3, 24, 160, dtype=DT[dtype], device="cuda")[::2, 1, 4:20, 32:]
+    b = torch.zeros(4, 2, 96, 40, dtype=DT[dtype], device="cuda")[:, 1, :, 8:24]
+    a.copy_(s["a"]), b.copy_(s["b"])
+    got = adapters.low_rank_add(y, x, a, b, s["ids"], s["scales"], out=out)
+    assert got is out and torch.equal(out, want)
+    assert (wide["out"][:, :200] == 7).all() and (wide["out"][:, 296:] == 7).all()
+    assert adapters.low_rank_add(y, x, a, b, s["ids"], s["scales"], out=y) is y and torch.equal(y, want)
+    assert (wide["y"][:, :64] == 7).all() and (wide["y"][:, 160:] == 7).all()
+    alone = make(6, tokens, 128, 96, 1, 16, dtype)
+    alone["scales"] = None
+    check(alone, adapters.low_rank_add(**alone), dtype)
+
+
+def test_rows_past_32_bits():
+    """Tokens and adapters whose rows lie more than 2^31 values apart."""
+    far = (1 << 30) + 8
+    s = make(7, 3, 64, 64, 2, 16, "bf16", [1, 0, 1])
+    want = adapters.low_rank_add(**s)
+    room = torch.empty(2 * far + 4096, dtype=torch.bfloat16, device="cuda")
+    y, x = room.as_strided((3, 64), (far, 1)), room.as_strided((3, 64), (far, 1), 64)
+    a = room.as_strided((2, 16, 64), (2 * far, 64, 1), 256)
+    b = room.as_strided((2, 64, 16), (2 * far, 16, 1), 2048)
+    for t, v in ((y, s["y"]), (x, s["x"]), (a, s["a"]), (b, s["b"])):
+        t.copy_(v)
+    assert torch.equal(adapters.low_rank_add(y, x, a, b, s["ids"], s["scales"]), want)
+    assert torch.equal(adapters.low_rank_add(y, x, a, b, s["ids"], s["scales"], out=y), want)
+
+
+@pytest.mark.parametrize("tokens,count", [(1, 4), (50, 20), (700, 5)])
+def test_same_bits_streams_and_graphs(tokens, count):
+    s = make(8, tokens, 640, 512, count, 32, "bf16")
+    want = adapters.low_rank_add(**s)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    on_side = adapters.low_rank_add(**s, stream=side)
+    side.synchronize()
+    assert torch.equal(on_side, want) and torch.equal(adapters.low_rank_add(**s), want)
+    # a captured step, on other inputs in each replay, its eager twin between them
+    out = torch.empty_like(s["y"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        adapters.low_rank_add(**s, out=out)
+    for seed in range(3):
+        new = make(20 + seed, tokens, 640, 512, count, 32, "bf16")
+        for k, v in new.items():
+            s[k].copy_(v)
+        graph.replay()
+        eager = adapters.low_rank_add(**new)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+
+
+def test_after_a_protected_projection():
+    """As a program uses it: the adapters added to the output of a checksum-protected layer of 1x1 maps."""
+    s = make(9, 24, 96, 160, 3, 16, "bf16")
+    w = (torch.randn(160, 96, 1, 1, generator=torch.Generator().manual_seed(1)) * 0.1).to("cuda", torch.bfloat16)
+    layer = ft.Layer(24, 96, 1, 1, 160, 1, 1, dtype="bf16", policy=ft.make_policy(repair="recompute"))
+    layer.encode_weights(w)
+    y = layer.empty_output()
+    layer.protected_fused(s["x"].reshape(layer.shape_d), w, y, (dict(n=5, m=17, x=0, y=0, kind="set", value=1e6),))
+    s["y"] = y.view(24, 160)
+    assert layer.read_report().status == ft.STATUS_CORRECTED
+    check(s, adapters.low_rank_add(**s), "bf16")
+
+
+def test_binding_refuses():
+    s = make(10, 6, 64, 64, 2, 16, "bf16")
+    bad = [("x", s["x"][:5]), ("x", s["x"].float()), ("a", s["a"][:, :, :56]), ("b", s["b"][:1]), ("b", s["b"][:, :, :8]),
+           ("ids", s["ids"].long()), ("ids", s["ids"][:5]), ("scales", s["scales"].double()), ("scales", s["scales"][:1]),
+           ("ids", s["ids"].cpu()), ("x", s["x"].t().contiguous().t()), ("y", s["y"].half())]
+    for k, v in bad:
+        with pytest.raises(ft.FtcnnError, match="low_rank_add"):
+            adapters.low_rank_add(**{**s, k: v})
+    for kw in (dict(out=s["y"][:5]), dict(out=s["y"].float()), dict(ranks=s["ids"]),
+               dict(workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(ft.FtcnnError, match="low_rank_add"):
+            adapters.low_rank_add(**s, **kw)
+    with pytest.raises(ft.FtcnnError, match="16 bytes"):
+        adapters.low_rank_add(**{**s, "x": torch.zeros(6, 72, dtype=torch.bfloat16, device="cuda")[:, 4:68]})
+    with pytest.raises(ft.FtcnnError, match="no backward"):
+        adapters.low_rank_add(**{**s, "x": s["x"].clone().requires_grad_()})
+    with torch.no_grad():
+        adapters.low_rank_add(**{**s, "x": s["x"].clone().requires_grad_()})
+    none = adapters.low_rank_add(s["y"][:0], s["x"][:0], s["a"], s["b"], s["ids"][:0])
+    assert none.shape == (0, 64)
