@@ -12,6 +12,8 @@ struct MassArgs {
     long long mass_stride;
     int blocks;                  // blocks of keys that the launch has for a sequence
     int head_parts, row_parts;   // workgroups that share a block's key heads, and its rows
+    FastDiv div_heads, div_rows, div_blocks;   // by head_parts, row_parts, blocks
+    bool near;                   // 32 tokens of the queries lie within 2^32 bytes
 };
 struct MassPlan {
     int dp;                      // head size the kernel is compiled for

@@ -146,22 +146,34 @@ MassPlan mass_plan(const ftcnn_mass_desc &d) {
     const long long rows = max_q * group;
     const int es = d.dtype == FTCNN_F32 ? 4 : 2;
     p.dp = d.dim <= 64 ? 64 : (d.dim <= 128 ? 128 : 256);
-    p.wide = rows > 16;
+    p.wide = rows > 64;
     const bool narrow = p.dp * es <= 256;
-    p.keys = p.wide ? (narrow ? 256 : 128) : (narrow ? 128 : 64);
     p.head_parts = p.row_parts = 1;
-    const long long blocks = (max_kv + p.keys - 1) / p.keys;
+    p.keys = narrow ? 32 : 16;
     if (p.wide) {
-        // four workgroups to a compute unit, so that long ones even out; parts of at most 2^28 bytes
-        const long long want = 4 * kComputeUnits, base = blocks * d.batch, room = (1LL << 26) / (d.batch * capacity);
-        auto share = [&](long long most, long long have) {
-            return (int)std::max(1LL, std::min({most, (want + have - 1) / have}));
+        // Parts of at most 2^28 bytes.  A key head is a workgroup's, and its rows are shared by so many that there are two
+        // workgroups to a compute unit, of two tiles of 64 rows at least, or eight, so that long ones even out, of eight
+        // tiles (two prompts of 8192 tokens 560 us, four 602; 512 tokens over 8704 keys, which have 32 tiles, 61 with four
+        // workgroups to a compute unit, 73 with eight).
+        const long long room = (1LL << 26) / (d.batch * capacity), tiles = (rows + 63) / 64;
+        auto split = [&](int keys) {
+            p.keys = keys;
+            p.head_parts = (int)std::max(1LL, std::min<long long>(d.kv_heads, room));
+            const long long base = (max_kv + keys - 1) / keys * d.batch * p.head_parts;
+            auto share = [&](long long want, long long least) { return std::min(tiles / least, (want * kComputeUnits + base - 1) / base); };
+            p.row_parts = (int)std::max(1LL, std::min(std::max(share(2, 2), share(8, 8)), room / p.head_parts));
+            return base * p.row_parts;
         };
-        p.head_parts = (int)std::max(1LL, std::min<long long>(share(d.kv_heads, base), room));
-        const long long tiles = (rows + 63) / 64;
-        p.row_parts = (int)std::max(1LL, std::min<long long>(share((tiles + 3) / 4, base * p.head_parts), room / p.head_parts));
+        // a wave has 64 keys where registers hold them (those prompts 582 us; 32 650), 32 where there are too few
+        // workgroups otherwise (3 x 257 tokens over 1257 keys, fp32, heads of 64: 27 us; 64 keys 37)
+        if (!narrow || split(256) < 2 * kComputeUnits) split(128);
         if (p.head_parts * p.row_parts > 1)
             p.bytes = up256((size_t)p.head_parts * p.row_parts * d.batch * capacity * sizeof(float));
+    }
+    const long long blocks = (max_kv + p.keys - 1) / p.keys;
+    if (!p.wide) {   // as many workgroups as are on the device at a time
+        p.blocks = (int)std::min(blocks * d.batch, (long long)kComputeUnits * (narrow ? 3 : 2));
+        return p;
     }
     // a workgroup goes on to block b + p.blocks
     const long long most = kMaxThreads / kThreads / ((long long)d.batch * p.head_parts * p.row_parts);
@@ -251,7 +263,7 @@ int ftcnn_attention_mass(const ftcnn_mass_desc *d, const void *q, const void *k_
     const MassPlan pl = mass_plan(*d);
     rc = check_workspace(what, pl.bytes, workspace);
     if (rc != FTCNN_OK) return rc;
-    const long long blocks = (long long)pl.blocks * d->batch * pl.head_parts * pl.row_parts;
+    const long long blocks = pl.wide ? (long long)pl.blocks * d->batch * pl.head_parts * pl.row_parts : pl.blocks;
     if (blocks > kMaxThreads / kThreads) return set_error(FTCNN_E_SHAPE, "%s: %lld workgroups", what, blocks);
     MassArgs m{};
     AttnArgs &t = m.t;
@@ -286,6 +298,10 @@ int ftcnn_attention_mass(const ftcnn_mass_desc *d, const void *q, const void *k_
     m.blocks = pl.blocks;
     m.head_parts = pl.head_parts;
     m.row_parts = pl.row_parts;
+    m.div_heads = fast_div((uint32_t)pl.head_parts);
+    m.div_rows = fast_div((uint32_t)pl.row_parts);
+    m.div_blocks = fast_div((uint32_t)pl.blocks);
+    m.near = d->q_stride[0] >= 0 && d->q_stride[0] < 1 << 24;
     FT_REQUESTS_HIP(d->dtype == FTCNN_F32 ? launch_mass_f32(pl, m, stream) : launch_mass_bf16(pl, m, stream), what);
     if (pl.bytes) FT_REQUESTS_HIP(launch_mass_join(pl, m, stream), "attention_mass: join");
     return FTCNN_OK;

@@ -89,6 +89,31 @@ def test_hints_shape_the_launch_only(dtype):
         check(s, call(s, max_q=hints[0], max_kv=hints[1]))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [40, 72, 200])
+@pytest.mark.parametrize("window,causal", [(0, True), (50, True), (0, False)])
+def test_lists_for_far_more_than_is_cached(dim, window, causal, dtype):
+    """Launches shaped for many keys: 64 of them to a wave, parts of many workgroups."""
+    new, length = [70, 1, 130, 64], [300, 90, 130, 700]
+    s = make(62, dtype, new, length, 4, 2, dim, 16)
+    with_lse(s, causal=causal, window=window)
+    wide = torch.full((4, 2000), -1, dtype=torch.int32, device="cuda")
+    wide[:, :s["lists"].shape[1]] = s["lists"]
+    s["lists"], s["mass"] = wide, torch.rand(4, 2000 * 16, device="cuda")
+    check(s, call(s, causal=causal, window=window), causal, window)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,most", [(70, 1), (130, 1), (200, 1), (70, 40)])
+def test_many_sequences(batch, most, dtype):
+    """More than a wave's lanes, many of them empty or without new tokens."""
+    rng = np.random.default_rng(batch)
+    new = rng.integers(1 if most == 1 else 0, most + 1, batch)
+    length = new * (rng.random(batch) < 0.7) * 1 + rng.integers(0, 2, batch) * rng.integers(0, 90, batch)
+    s = with_lse(make(63, dtype, new.tolist(), length.tolist(), 4, 2, 16, 8))
+    check(s, call(s, max_q=most, max_kv=int(length.max())))
+
+
 def test_single_tokens_need_no_starts():
     s = with_lse(make(51, "bf16", [1, 1, 1], [30, 200, 0], 8, 2, 128, 16))
     assert torch.equal(call(s, starts=False), call(s, max_q=1))
