@@ -10,18 +10,23 @@ struct LowRankArgs {
     void *out;
     const float *scales;          // NULL: 1
     const int32_t *ranks, *ids;   // ranks NULL: all of `rank`
-    float *part;                  // [splits][tokens][rank]: s A x of each range of channels
+    float *low;                   // [splits][tokens][rank]: s A x of each range of channels
+    int4 *records;                // grouped tokens: (adapter, first, how many, 0) of each tile
+    int32_t *grouped, *count;     // the tokens, and how many tiles
     long long xs, ys, os;         // elements between tokens
     long long as[2], bs[2];       // elements between adapters, rows
     int tokens, ch, m, adapters, rank;
-    int splits;                   // ranges of channels
-    int tiles, ways;              // tiles of tokens; workgroups that share a tile's adapters, in either launch
-    int expand_ways, columns;     // outputs of a workgroup of the second launch
+    int groups, splits;           // groups of rows of A, and ranges of channels, of workgroups of their own
+    int ways, expand_ways;        // workgroups that share a tile's adapters, in either launch
+    int columns, tiles, together; // outputs of a wave of the second launch; tiles, and those of a workgroup of it
+    FastDiv div_groups, div_splits, div_ways, div_expand_ways, div_spans;
 };
 struct LowRankPlan {
+    bool grouped;                 // tokens are grouped by adapter first
     int tile;                     // tokens of a tile
-    int splits, tiles, ways, expand_ways, columns;
-    size_t bytes;
+    int blocks;                   // rows of A of a workgroup, in 16
+    int tiles, groups, splits, ways, expand_ways, columns, together, spans;   // spans of outputs of the second's workgroups
+    size_t records, order, count, bytes;   // workspace: after the products
 };
 LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d);
 hipError_t launch_low_rank(int dtype, const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st);

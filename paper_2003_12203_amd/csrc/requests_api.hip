@@ -80,9 +80,9 @@ int check_low_rank(const ftcnn_low_rank_desc *d) {
     if (d->tokens > kMaxRows) return set_error(FTCNN_E_SHAPE, "%s: more than 2^30 tokens", what);
     if (d->tokens) {
         const LowRankPlan p = low_rank_plan(*d);
-        const long long one = (long long)p.tiles * p.ways * p.splits;
-        const long long two = (long long)p.tiles * p.expand_ways * ((d->m + p.columns - 1LL) / p.columns);
-        if (std::max(one, two) > kMaxThreads / kThreads) return set_error(FTCNN_E_SHAPE, "%s: %lld workgroups", what, std::max(one, two));
+        const long long one = (long long)p.tiles * p.ways * p.splits * p.groups, two = (long long)p.tiles * p.expand_ways * p.spans;
+        if (std::max(2 * one, two) > kMaxThreads / kThreads)
+            return set_error(FTCNN_E_SHAPE, "%s: %lld and %lld workgroups", what, one, two);
     }
     return FTCNN_OK;
 }
@@ -217,7 +217,13 @@ int ftcnn_low_rank_add(const ftcnn_low_rank_desc *d, const void *y, const void *
     g.scales = scales;
     g.ranks = ranks;
     g.ids = ids;
-    g.part = static_cast<float *>(workspace);
+    char *ws = static_cast<char *>(workspace);
+    g.low = static_cast<float *>(workspace);
+    if (pl.grouped) {
+        g.records = reinterpret_cast<int4 *>(ws + pl.records);
+        g.grouped = reinterpret_cast<int32_t *>(ws + pl.order);
+        g.count = reinterpret_cast<int32_t *>(ws + pl.count);
+    }
     g.xs = d->x_stride;
     g.ys = d->y_stride;
     g.os = d->out_stride;
@@ -230,11 +236,18 @@ int ftcnn_low_rank_add(const ftcnn_low_rank_desc *d, const void *y, const void *
     g.m = d->m;
     g.adapters = d->adapters;
     g.rank = d->rank;
+    g.groups = pl.groups;
     g.splits = pl.splits;
     g.tiles = pl.tiles;
+    g.together = pl.together;
+    g.div_splits = fast_div((uint32_t)pl.splits);
     g.ways = pl.ways;
     g.expand_ways = pl.expand_ways;
     g.columns = pl.columns;
+    g.div_groups = fast_div((uint32_t)pl.groups);
+    g.div_ways = fast_div((uint32_t)pl.ways);
+    g.div_expand_ways = fast_div((uint32_t)pl.expand_ways);
+    g.div_spans = fast_div((uint32_t)pl.spans);
     FT_REQUESTS_HIP(launch_low_rank(d->dtype, pl, g, stream), what);
     return FTCNN_OK;
 }
