@@ -52,7 +52,8 @@ struct TileTokens {
 template <int TILE, bool GROUPED, typename F>
 __device__ __forceinline__ void each_adapter(const LowRankArgs &a, int tile, int way, int ways, F f) {
     if constexpr (GROUPED) {
-        if (tile >= *a.count) return;
+        const int part = (int)div_by(tile, a.div_slots);
+        if (tile - part * a.slots >= a.counts[part]) return;
         const int4 r = a.records[tile];
         f(__builtin_amdgcn_readfirstlane(r.x), TileTokens{r.y, r.z, 0, a.grouped});
     } else {
@@ -74,44 +75,39 @@ __device__ __forceinline__ void each_adapter(const LowRankArgs &a, int tile, int
     }
 }
 
-constexpr int kGroup = 1024;   // threads of group_kernel
+constexpr int kGroup = 1024, kPart = 2 * kGroup;   // threads of group_kernel; tokens of a workgroup of it
 
-// The tokens of each adapter together, in tiles of `tile`: grouped[] has them one adapter's after the other's (those without one
-// last), records[] (adapter, first of grouped, how many, 0) for each tile, *count how many.  One workgroup.  In which order an
-// adapter's tokens come hangs on timing, and nothing on that: a row's products are its own.
+// The tokens of each adapter together, in tiles of `tile`, of every part of kPart tokens for itself: grouped[] has them one
+// adapter's after the other's (those without one last), records[] (adapter, first of grouped, how many, 0) for each tile, slots
+// of them a part, counts[] how many.  A workgroup a part.  In which order an adapter's tokens come hangs on timing, and nothing
+// on that: a row's products are its own.
 __global__ __launch_bounds__(kGroup) void group_kernel(LowRankArgs a, int tile) {
     extern __shared__ __align__(16) int room[];
     const int bins = a.adapters + 1, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int t0 = blockIdx.x * kPart, end = min(t0 + kPart, a.tokens);
     int *tokens_of = room, *tiles_of = room + bins;   // counts, then where they begin
     __shared__ int sums[2][kGroup / 64];
+    int x[2], at[2];   // this lane's tokens: the bin, the place in it
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t = t0 + i * kGroup + tid, id = t < end ? a.ids[t] : -1;
+        x[i] = (unsigned)id < (unsigned)a.adapters ? id : a.adapters;
+    }
     for (int i = tid; i < bins; i += kGroup) tokens_of[i] = 0;
     __syncthreads();
-    auto bin = [&](int t) {
-        const int id = a.ids[t];
-        return (unsigned)id < (unsigned)a.adapters ? id : a.adapters;
-    };
-    // Adds the lanes to their bins' counts and returns what was there and in lower lanes: a wave whose tokens have one or two adapters (a
-    // prompt's) with one addition for each.
-    auto add = [&](int x, bool on) {
-        int at = 0;
-        unsigned long long left = __ballot(on);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (left) {
-                const int first = __builtin_ctzll(left), theirs = __builtin_amdgcn_readlane(x, first);
-                const unsigned long long same = __ballot(on && x == theirs) & left;
-                int base = 0;
-                if (lane == first) base = atomicAdd(&tokens_of[theirs], __popcll(same));
-                base = __builtin_amdgcn_readlane(base, first);
-                if (same >> lane & 1) at = base + __popcll(same & ((1ull << lane) - 1));
-                left &= ~same;
-            }
-        if (left >> lane & 1) at = atomicAdd(&tokens_of[x], 1);
-        return at;
-    };
-    for (int t0 = 0; t0 < a.tokens; t0 += kGroup) {
-        const int t = t0 + tid;
-        add(t < a.tokens ? bin(t) : 0, t < a.tokens);
+    for (int i = 0; i < 2; ++i) {
+        const bool on = t0 + i * kGroup + tid < end;
+        // a wave whose tokens have one adapter (a prompt's), or many of them the first one's, does one addition for those
+        const unsigned long long left = __ballot(on);
+        if (left == 0) continue;
+        const int theirs = __builtin_amdgcn_readlane(x[i], __builtin_ctzll(left));
+        const unsigned long long same = __ballot(on && x[i] == theirs);
+        int base = 0;
+        if (lane == 0) base = atomicAdd(&tokens_of[theirs], __popcll(same));
+        if (on && x[i] != theirs) at[i] = atomicAdd(&tokens_of[x[i]], 1);
+        base = __builtin_amdgcn_readfirstlane(base);
+        if (on && x[i] == theirs) at[i] = base + __popcll(same & ((1ull << lane) - 1));
     }
     __syncthreads();
     // where each bin's tokens and tiles begin: thread t has `run` bins from run * t on
@@ -123,9 +119,9 @@ __global__ __launch_bounds__(kGroup) void group_kernel(LowRankArgs a, int tile) 
     }
     int tokens_to = tokens, tiles_to = tiles;
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) {
-        const int p = __shfl_up(tokens_to, x), q = __shfl_up(tiles_to, x);
-        if (lane >= x) {
+    for (int y = 1; y < 64; y *= 2) {
+        const int p = __shfl_up(tokens_to, y), q = __shfl_up(tiles_to, y);
+        if (lane >= y) {
             tokens_to += p;
             tiles_to += q;
         }
@@ -153,21 +149,21 @@ __global__ __launch_bounds__(kGroup) void group_kernel(LowRankArgs a, int tile) 
         tiles_to += (n + tile - 1) / tile;
     }
     __syncthreads();
-    for (int i = tid; i < total; i += kGroup) {   // the bin of tile i: the last that begins at or before it, and is not empty
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int t = t0 + i * kGroup + tid;
+        if (t < end) a.grouped[t0 + tokens_of[x[i]] + at[i]] = t;
+    }
+    if (tid == 0) a.counts[blockIdx.x] = total;
+    for (int i = tid; i < total; i += kGroup) {   // the bin of tile i: the last that begins at or before it
         int lo = 0, hi = bins;
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
             if (tiles_of[mid] <= i) lo = mid;
             else hi = mid;
         }
-        const int first = tokens_of[lo] + (i - tiles_of[lo]) * tile, end = lo + 1 < bins ? tokens_of[lo + 1] : a.tokens;
-        a.records[i] = make_int4(lo < a.adapters ? lo : -1, first, min(tile, end - first), 0);
-    }
-    if (tid == 0) *a.count = total;
-    __syncthreads();
-    for (int t0 = 0; t0 < a.tokens; t0 += kGroup) {
-        const int t = t0 + tid, at = add(t < a.tokens ? bin(t) : 0, t < a.tokens);
-        if (t < a.tokens) a.grouped[at] = t;
+        const int first = tokens_of[lo] + (i - tiles_of[lo]) * tile, next = lo + 1 < bins ? tokens_of[lo + 1] : end - t0;
+        a.records[(long long)blockIdx.x * a.slots + i] = make_int4(lo < a.adapters ? lo : -1, t0 + first, min(tile, next - first), 0);
     }
 }
 
@@ -180,7 +176,7 @@ constexpr int kShrinkWaves = 8;
 // The products of a tile's tokens with 16 NB rows of their adapter's A.  A workgroup's waves share its channels, each keeps AHEAD
 // chunks of every row on their way while it multiplies as many, and their sums are added in LDS.  Rows of tokens that have another adapter,
 // and those past the rank, are read as ones that are there: their products go nowhere.
-template <typename T, int MT, int NB, bool GROUPED>
+template <typename T, int MT, int NB>
 __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(LowRankArgs a) {
     using C = Chunk<T>;
     constexpr int W = kShrinkWaves, TILE = 16 * MT, RANK = 16 * NB, AHEAD = MT + NB <= 3 ? 4 : (MT + NB <= 6 ? 2 : 1);
@@ -195,7 +191,7 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(LowRankArgs a
     const int chunks = (a.ch + C::VALUES - 1) / C::VALUES, whole = a.ch / C::VALUES, part = split * W + w, parts = a.splits * W;
     const int blocks = max((whole / 4 - part + parts - 1) / parts, 0), groups = blocks * (4 / AHEAD);
     const auto chunk_of = [&](int g) { return (part + g / (4 / AHEAD) * parts) * 4 + g % (4 / AHEAD) * AHEAD; };
-    each_adapter<TILE, GROUPED>(a, (int)x3, way, a.ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
+    each_adapter<TILE, false>(a, (int)x3, way, a.ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
         if (adapter < 0) return;
         const int rank = used_rank(a, adapter);
         const T *xr[MT], *ar[NB];
@@ -286,6 +282,115 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(LowRankArgs a
     });
 }
 
+// The same for grouped tokens, of which there are many: rows of tokens and of A come into LDS in pieces of 256 bytes, whole lines of
+// neighbouring lanes (a load in the order of the operands touches sixteen lines for each 256 bytes of it, and the first-level cache
+// looks one up a cycle), DEPTH - 1 pieces ahead, and every wave multiplies 64 bytes of each row of a piece.
+template <typename T, int MT, int NB> struct Ring {
+    static constexpr int ROWS = 16 * (MT + NB), PIECE = 256, STAGE = ROWS * PIECE;
+    static constexpr int LOADS = ROWS / 16;                                  // of a wave and stage, four rows each
+    static constexpr int DEPTH = 81920 / STAGE < 8 ? 81920 / STAGE : 8, LDS = DEPTH * STAGE;   // two workgroups to a compute unit
+    static_assert(DEPTH >= 2 && (DEPTH - 2) * LOADS < 64 && 4 * 16 * MT * 16 * NB * 4 <= LDS, "the waits count to 63; the sums fit");
+};
+template <int N> __device__ __forceinline__ void wait_all_but() {   // all but the last N loads of this wave have landed
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+}
+
+template <typename T, int MT, int NB>
+__global__ __launch_bounds__(256) void shrink_ring_kernel(LowRankArgs a) {
+    using C = Chunk<T>;
+    using R = Ring<T, MT, NB>;
+    constexpr int EU = C::EU, TILE = 16 * MT, RANK = 16 * NB, PER = 16 * EU;   // values of a piece of a row
+    extern __shared__ __align__(1024) unsigned char ring[];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, h = lane >> 4;
+    typedef __attribute__((address_space(3))) unsigned char lds_byte;
+    const unsigned ring_at = (unsigned)(uintptr_t)(lds_byte *)ring;
+    const unsigned x1 = div_by(blockIdx.x, a.div_groups), x2 = div_by(x1, a.div_splits);
+    const int r0 = (int)(blockIdx.x - x1 * a.groups) * RANK, split = (int)(x1 - x2 * a.splits);
+    const int of = (int)div_by(x2, a.div_slots);
+    if ((int)x2 - of * a.slots >= a.counts[of]) return;
+    const int4 record = a.records[x2];
+    const int adapter = __builtin_amdgcn_readfirstlane(record.x);
+    if (adapter < 0) return;
+    const TileTokens tokens{record.y, record.z, 0, a.grouped};
+    const int rank = used_rank(a, adapter);
+    // this workgroup's pieces of every row
+    const int pieces = (a.ch + PER - 1) / PER, each = (int)div_by(pieces, a.div_splits), more = pieces - each * a.splits;
+    const int p0 = each * split + min(split, more), count = each + (split < more ? 1 : 0);
+    // this wave's loads: four rows each, tokens first, then A; the unit of a row that belongs at this lane's place.  Rows of no token,
+    // and those past the rank, are others' that are there: their products go nowhere.
+    const char *from[R::LOADS];
+    int unit[R::LOADS];
+#pragma unroll
+    for (int i = 0; i < R::LOADS; ++i) {
+        const int row = 4 * (4 * i + w) + h;   // 4 i + w: of 4 (MT + NB) loads
+        unit[i] = n16 ^ (row & 15);
+        const T *at = row < TILE ? static_cast<const T *>(a.x) + tokens.token(row) * a.xs
+                                 : static_cast<const T *>(a.a) + adapter * a.as[0] + min(r0 + row - TILE, a.rank - 1) * a.as[1];
+        from[i] = reinterpret_cast<const char *>(at + (long long)p0 * PER) + unit[i] * 16;
+    }
+    auto issue = [&](int t) __attribute__((always_inline)) {   // piece p0 + t
+        const unsigned to = ring_at + t % R::DEPTH * R::STAGE + w * 1024;
+        const int left = a.ch - (p0 + t) * PER;   // values of the row from this piece on
+        if (left >= PER) {
+#pragma unroll
+            for (int i = 0; i < R::LOADS; ++i) load_to_lds(from[i] + (long long)t * 256, to + i * 4096);
+        } else {
+#pragma unroll
+            for (int i = 0; i < R::LOADS; ++i)
+                if (unit[i] * EU < left) load_to_lds(from[i] + (long long)t * 256, to + i * 4096);
+        }
+    };
+    f32x4 acc[MT][NB];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    wait_loads();   // what came before is not counted below
+    for (int t = 0; t < R::DEPTH - 1 && t < count; ++t) issue(t);
+    for (int t = 0; t < count; ++t) {
+        if (t + R::DEPTH - 1 <= count) wait_all_but<(R::DEPTH - 2) * R::LOADS>();
+        else wait_loads();
+        tile_barrier();   // piece t has landed, and nobody reads piece t - 1 any more
+        if (t + R::DEPTH - 1 < count) issue(t + R::DEPTH - 1);
+        const unsigned char *at = ring + t % R::DEPTH * R::STAGE + (((4 * w + h) ^ n16) << 4) + n16 * 256;
+        uint4 xf[MT], af[NB];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xf[i] = *reinterpret_cast<const uint4 *>(at + 16 * i * 256);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) af[j] = *reinterpret_cast<const uint4 *>(at + (TILE + 16 * j) * 256);
+        if ((p0 + t + 1) * PER > a.ch && (p0 + t) * PER + (4 * w + h) * EU >= a.ch) {   // past the channels: LDS holds anything
+#pragma unroll
+            for (int i = 0; i < MT; ++i) xf[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) af[j] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = product<T>(xf[i], af[j], acc[i][j]);
+    }
+    __syncthreads();
+    float *sums = reinterpret_cast<float *>(ring);   // [4][TILE][RANK]
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[(w * TILE + 16 * i + 4 * h + e) * RANK + 16 * j + n16] = acc[i][j][e];
+    __syncthreads();
+    const float s = a.scales ? a.scales[adapter] : 1.0f;
+    for (int i = threadIdx.x; i < TILE * RANK; i += 256) {
+        const int t = i / RANK, r = r0 + i % RANK;
+        if (!tokens.has(t) || r >= a.rank) continue;
+        float v = sums[i];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) v += sums[k * TILE * RANK + i];
+        a.low[((long long)split * a.tokens + tokens.token(t)) * a.rank + r] = r < rank ? s * v : 0.0f;
+    }
+}
+
 // Unit k..k + EU of a row of B, without what lies past the rank that is used.
 template <typename T> __device__ __forceinline__ uint4 within_rank(uint4 v, int k, int rank) {
     constexpr int EU = 16 / sizeof(T);
@@ -301,10 +406,6 @@ template <typename T> union Unit {
     uint4 q;
     T e[16 / sizeof(T)];
 };
-template <typename T> union Row16 {
-    uint4 q[sizeof(T)];
-    T e[16];
-};
 __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(uint16_t v) { return bf16_bits_to_f32(v); }
 __device__ __forceinline__ void narrow(float &d, float v) { d = v; }
@@ -313,16 +414,21 @@ __device__ __forceinline__ void narrow(uint16_t &d, float v) { d = f32_to_bf16_r
 // The product is O^T = B H^T: a lane has a token, and of each of four blocks of 16 outputs the rows 4 h + e.
 // Row 4 g + e of block q is output 16 g + 4 q + e, so that a lane's 16 values are neighbours and four lanes hold 64
 // outputs of a token.  A wave has its tile's h in registers and goes over some outputs, 64 at a time, those of y and B on their
-// way while the ones before are multiplied.
+// way while the ones before are multiplied.  The products go through LDS, which each wave has for itself, so that y and the
+// output are read and written in whole lines (see Ring).
 //
 // bf16: h is the sum of two bf16 values (an error of 2^-17 of it; rounded to one, its products would be off by as
 // much as the outputs' own rounding).
 template <typename T, int MT, int RC, bool GROUPED>
 __global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
     using C = Chunk<T>;
-    constexpr int EU = C::EU, TILE = 16 * MT, PLANES = sizeof(T) == 2 ? 2 : 1, SZ = (int)sizeof(T);
+    constexpr int EU = C::EU, TILE = 16 * MT, PLANES = sizeof(T) == 2 ? 2 : 1;
+    constexpr int LPR = 64 / EU, RPL = 64 / LPR, PASSES = TILE / RPL;   // lanes of a row's 64 outputs; rows of a load; loads
+    constexpr int PITCH = 68;   // floats: 16 rows begin at different banks
+    __shared__ __align__(16) float room[4][TILE * PITCH];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n16 = lane & 15, h = lane >> 4;
+    const int n16 = lane & 15, h = lane >> 4, row = lane / LPR, col = lane % LPR * EU;
+    float *mine = room[w];
     const unsigned x1 = div_by(blockIdx.x, a.div_spans), x2 = div_by(x1, a.div_expand_ways);
     const int way = (int)(x1 - x2 * a.expand_ways);
     // a workgroup's waves have `together` tiles (one or four), which share the loads of B, and one or four spans of outputs
@@ -345,38 +451,39 @@ __global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
         }
         const int rank = used_rank(a, adapter);
         const T *bt = static_cast<const T *>(a.b) + adapter * a.bs[0];
-        // workgroups begin at different places of their span: rows of y often lie a power of two apart, and 64 of its
-        // columns in all rows at one memory channel
-        const int steps = (m1 - m0 + 63) / 64, turn = (int)(x2 % (unsigned)steps);
-        auto place = [&](int i) __attribute__((always_inline)) { return m0 + 64 * (i + turn < steps ? i + turn : i + turn - steps); };
-        bool on[MT];
-        const T *yt[MT];
-        T *ot[MT];
+        const int steps = (m1 - m0 + 63) / 64;
         uint4 low[MT][RC][PLANES];   // (of other tokens any values: their products go nowhere)
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            on[i] = tokens.has(16 * i + n16);
             const long long t = tokens.token(16 * i + n16);
-            yt[i] = static_cast<const T *>(a.y) + t * a.ys + 16 * h;
-            ot[i] = static_cast<T *>(a.out) + t * a.os + 16 * h;
 #pragma unroll
             for (int c = 0; c < RC; ++c) {
                 const int k = c * C::VALUES + h * EU;
                 float v[EU];
 #pragma unroll
                 for (int e = 0; e < EU; ++e) v[e] = 0.0f;
-                if (k < a.rank)
-                    for (int s = 0; s < a.splits; ++s) {
-                        const float4 *from = reinterpret_cast<const float4 *>(a.low + (s * (long long)a.tokens + t) * a.rank + k);
+                if (k < a.rank) {
+                    const float *from = a.low + t * a.rank + k;
+                    const long long step = (long long)a.tokens * a.rank;
+                    for (int s = 0; s < a.splits; s += 4) {   // four ranges' loads at a time
+                        float4 f[4][EU / 4];
 #pragma unroll
-                        for (int e = 0; e < EU; e += 4) {
-                            const float4 f = from[e / 4];
-                            v[e] += f.x;
-                            v[e + 1] += f.y;
-                            v[e + 2] += f.z;
-                            v[e + 3] += f.w;
-                        }
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int e = 0; e < EU / 4; ++e)
+                                f[j][e] = reinterpret_cast<const float4 *>(from + min(s + j, a.splits - 1) * step)[e];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (s + j < a.splits)
+#pragma unroll
+                                for (int e = 0; e < EU; e += 4) {
+                                    v[e] += f[j][e / 4].x;
+                                    v[e + 1] += f[j][e / 4].y;
+                                    v[e + 2] += f[j][e / 4].z;
+                                    v[e + 3] += f[j][e / 4].w;
+                                }
                     }
+                }
                 Unit<T> hi, lo;
 #pragma unroll
                 for (int e = 0; e < EU; ++e) {
@@ -388,39 +495,64 @@ __global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
                 if constexpr (PLANES == 2) low[i][c][PLANES - 1] = lo.q;
             }
         }
-        struct Stage {
-            Row16<T> y[MT];
-            uint4 b[RC][4];
+        bool on[PASSES];   // rows of y and the output that this lane reads and writes
+        const T *yt[PASSES];
+        T *ot[PASSES];
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            on[p] = tokens.has(p * RPL + row);
+            const long long t = tokens.token(p * RPL + row);
+            yt[p] = static_cast<const T *>(a.y) + t * a.ys;
+            ot[p] = static_cast<T *>(a.out) + t * a.os;
+        }
+        constexpr bool B_AHEAD = RC <= 2;   // (more would leave one wave to a SIMD)
+        struct Ahead {
+            uint4 b[B_AHEAD ? RC : 1][4];
         };
-        auto load = [&](Stage &s, int i) __attribute__((always_inline)) {
-            const int m = place(i);
-#pragma unroll
-            for (int c = 0; c < RC; ++c)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int row = m + 16 * (n16 >> 2) + 4 * q + (n16 & 3), k = c * C::VALUES + h * EU;
-                    // rows past the last: that one, for nobody; past the rank: zero, as h is
-                    s.b[c][q] = *reinterpret_cast<const uint4 *>(bt + min(row, m1 - 1) * a.bs[1] + min(k, a.rank - EU));
-                }
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int u = 0; u < SZ; ++u)
-                    s.y[t].q[u] = *reinterpret_cast<const uint4 *>(yt[t] + min(m + u * EU, m1 - EU - 16 * h));
+        struct Rows {
+            Unit<T> y[PASSES];
         };
-        auto multiply = [&](Stage &s, int i) __attribute__((always_inline)) {
-            const int m = place(i);
+        auto load_b = [&](uint4 (&to)[4], int c, int m) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = m + 16 * (n16 >> 2) + 4 * q + (n16 & 3), k = c * C::VALUES + h * EU;
+                // rows past the last: that one, for nobody; past the rank: zero, as h is
+                to[q] = *reinterpret_cast<const uint4 *>(bt + min(r, m1 - 1) * a.bs[1] + min(k, a.rank - EU));
+            }
+        };
+        // (of steps past the last: that one again, so that no load is under a condition)
+        auto load_ahead = [&](Ahead &s, int i) __attribute__((always_inline)) {
+            if constexpr (B_AHEAD) {
+#pragma unroll
+                for (int c = 0; c < RC; ++c) load_b(s.b[c], c, m0 + 64 * min(i, steps - 1));
+            }
+        };
+        auto load_rows = [&](Rows &s, int i) __attribute__((always_inline)) {
+            const int m = min(m0 + 64 * min(i, steps - 1) + col, m1 - EU);
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) s.y[p].q = *reinterpret_cast<const uint4 *>(yt[p] + m);
+        };
+        auto multiply = [&](const Rows &s, const Ahead &ahead, int i) __attribute__((always_inline)) {
+            const int m = m0 + 64 * i;
             f32x4 acc[4][MT];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
                 for (int t = 0; t < MT; ++t) acc[q][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            uint4 bf[B_AHEAD ? 1 : RC][4];
+            if constexpr (!B_AHEAD) {
+#pragma unroll
+                for (int c = 0; c < RC; ++c) load_b(bf[c], c, m);
+            }
 #pragma unroll
             for (int c = 0; c < RC; ++c) {
                 const int k = c * C::VALUES + h * EU;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const uint4 b = rank < RC * C::VALUES ? within_rank<T>(s.b[c][q], k, rank) : s.b[c][q];
+                    uint4 b;
+                    if constexpr (B_AHEAD) b = ahead.b[c][q];
+                    else b = bf[c][q];
+                    if (rank < RC * C::VALUES) b = within_rank<T>(b, k, rank);
 #pragma unroll
                     for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -428,45 +560,61 @@ __global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
                 }
             }
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                Row16<T> v;
+            for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) narrow(v.e[e], widen(s.y[t].e[e]) + acc[e / 4][t][e % 4]);
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<f32x4 *>(mine + (16 * t + n16) * PITCH + 16 * h + 4 * q) = acc[q][t];
+            // (a wave's own LDS operations are in order)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int u = 0; u < SZ; ++u)
-                    if (on[t] && m + 16 * h + u * EU < m1) *reinterpret_cast<uint4 *>(ot[t] + m + u * EU) = v.q[u];
+            for (int p = 0; p < PASSES; ++p) {
+                const float *at = mine + (p * RPL + row) * PITCH + col;
+                float add[EU];
+#pragma unroll
+                for (int e = 0; e < EU; e += 4) *reinterpret_cast<f32x4 *>(add + e) = *reinterpret_cast<const f32x4 *>(at + e);
+                Unit<T> v;
+#pragma unroll
+                for (int e = 0; e < EU; ++e) narrow(v.e[e], widen(s.y[p].e[e]) + add[e]);
+                if (on[p] && m + col < m1) *reinterpret_cast<uint4 *>(ot[p] + m + col) = v.q;
             }
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_wave_barrier();
         };
-        Stage s0, s1;
-        load(s0, 0);
-        int i = 0;
-        for (; i + 2 < steps; i += 2) {
-            load(s1, i + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(s0, i);
-            load(s0, i + 2);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(s1, i + 1);
-        }
-        if (i + 1 < steps) {
-            load(s1, i + 1);
-            multiply(s0, i);
-            multiply(s1, i + 1);
-        } else {
-            multiply(s0, i);
+        Ahead b0, b1;
+        Rows y0, y1, y2, y3;   // two steps ahead, B one
+        load_ahead(b0, 0);
+        load_rows(y0, 0);
+        load_rows(y1, 1);
+        for (int i = 0; i < steps; i += 4) {
+            auto step = [&](int j, Rows &now, Rows &later, Ahead &b, Ahead &next) __attribute__((always_inline)) {
+                load_ahead(next, i + j + 1);
+                load_rows(later, i + j + 2);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(now, b, i + j);
+            };
+            step(0, y0, y2, b0, b1);
+            if (i + 1 >= steps) break;
+            step(1, y1, y3, b1, b0);
+            if (i + 2 >= steps) break;
+            step(2, y2, y0, b0, b1);
+            if (i + 3 >= steps) break;
+            step(3, y3, y1, b1, b0);
         }
     });
 }
 
 template <typename T, int MT, int NB, bool GROUPED> hipError_t shrink_go(const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
-    constexpr int LDS = kShrinkWaves * 16 * MT * 16 * NB * (int)sizeof(float);
-    auto kernel = shrink_kernel<T, MT, NB, GROUPED>;
+    constexpr int LDS = GROUPED ? Ring<T, MT, NB>::LDS : kShrinkWaves * 16 * MT * 16 * NB * (int)sizeof(float);
+    void (*kernel)(LowRankArgs);
+    if constexpr (GROUPED) kernel = shrink_ring_kernel<T, MT, NB>;
+    else kernel = shrink_kernel<T, MT, NB>;
     if constexpr (LDS > 65536) {
         static std::atomic<uint64_t> raised{0};   // devices whose limit is raised for this kernel
         const hipError_t err = raise_lds_limit(reinterpret_cast<const void *>(kernel), LDS, raised);
         if (err != hipSuccess) return err;
     }
-    kernel<<<(unsigned)pl.tiles * pl.ways * pl.splits * pl.groups, 64 * kShrinkWaves, LDS, st>>>(a);
+    kernel<<<(unsigned)pl.tiles * pl.ways * pl.splits * pl.groups, GROUPED ? 256 : 64 * kShrinkWaves, LDS, st>>>(a);
     return hipGetLastError();
 }
 template <typename T, int MT, bool GROUPED> hipError_t go(const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
@@ -499,7 +647,14 @@ LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d) {
     p.grouped = d.tokens >= 512 && d.adapters > 1 && d.adapters < kMaxBins;
     // two tiles of 16 together where they fill the device and adapters have as many tokens
     p.tile = d.tokens >= 32 * kComputeUnits / 2 && d.tokens / d.adapters >= 32 ? 32 : 16;
-    p.tiles = (d.tokens + p.tile - 1) / p.tile + (p.grouped ? std::min(d.adapters, d.tokens) : 0);
+    p.tiles = (d.tokens + p.tile - 1) / p.tile;
+    if (p.grouped) {
+        // a part's tiles: every bin (an adapter, or none) has one that is not full at most, and all of them are full up to one
+        p.parts = (d.tokens + kPart - 1) / kPart;
+        p.slots = (std::min(kPart, d.tokens) + p.tile - 1) / p.tile + std::min(d.adapters, kPart);
+        p.slots = (p.slots + 3) / 4 * 4;   // the second launch's workgroups have four tiles of a part
+        p.tiles = p.parts * p.slots;
+    }
     const long long most = p.grouped ? 1 : std::max(1, std::min(p.tile, d.adapters));
     auto share = [&](long long want, long long have) { return (int)std::max(1LL, std::min(most, want / std::max(1LL, have))); };
     // rows of A together where tiles fill the device, apart where they do not
@@ -510,30 +665,30 @@ LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d) {
     p.ways = share(2 * kComputeUnits, (long long)p.tiles * p.groups);
     // ranges of channels where there are too few workgroups still: four chunks of 64 bytes a wave at least
     const long long chunks = ((long long)d.ch * (d.dtype == FTCNN_F32 ? 4 : 2) + 63) / 64;
-    p.splits = (int)std::max(1LL, std::min(chunks / (4 * kShrinkWaves), 2LL * kComputeUnits / ((long long)p.tiles * p.groups * p.ways)));
-    // outputs of a wave: as many as leave eight waves to a compute unit
+    p.splits = (int)std::max(1LL, std::min(chunks / (4 * kShrinkWaves), (p.grouped ? 1LL : 2LL) * kComputeUnits / ((long long)p.tiles * p.groups * p.ways)));
+    // The second launch: as many spans of 64 outputs as fill two workgroups to a compute unit, and no second round of them.
     const long long blocks = (d.m + 63) / 64;
-    p.expand_ways = share(8 * kComputeUnits, p.tiles * ((blocks + 3) / 4));
-    const long long waves = p.tiles * p.expand_ways * blocks;
-    const long long each = std::max(1LL, std::min(blocks, waves / (8LL * kComputeUnits)));
-    p.together = p.tiles >= 64 ? 4 : 1;
-    const long long of_group = each * (4 / p.together);
+    p.together = p.grouped || p.tiles >= 64 ? 4 : 1;
+    p.expand_ways = share(2 * kComputeUnits, p.tiles);
+    const long long rows_of = (p.tiles + p.together - 1) / p.together * (long long)p.expand_ways, wide = 4 / p.together;
+    const long long spans = std::max(1LL, std::min((blocks + wide - 1) / wide, 2 * kComputeUnits / rows_of));
+    const long long each = (blocks + spans * wide - 1) / (spans * wide);
     p.columns = (int)(64 * each);
-    p.spans = (int)((blocks + of_group - 1) / of_group);
+    p.spans = (int)((blocks + each * wide - 1) / (each * wide));
     auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
     p.records = up((size_t)p.splits * d.tokens * d.rank * sizeof(float));
     p.bytes = p.records;
     if (p.grouped) {
         p.order = p.records + up((size_t)p.tiles * sizeof(int4));
         p.count = p.order + up((size_t)d.tokens * sizeof(int32_t));
-        p.bytes = p.count + 256;
+        p.bytes = p.count + up(p.parts * sizeof(int32_t));
     }
     return p;
 }
 
 hipError_t launch_low_rank(int dtype, const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
     if (pl.grouped) {
-        group_kernel<<<1, kGroup, 2 * (a.adapters + 1) * sizeof(int), st>>>(a, pl.tile);
+        group_kernel<<<pl.parts, kGroup, 2 * (a.adapters + 1) * sizeof(int), st>>>(a, pl.tile);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
     }

@@ -222,7 +222,9 @@ int ftcnn_low_rank_add(const ftcnn_low_rank_desc *d, const void *y, const void *
     if (pl.grouped) {
         g.records = reinterpret_cast<int4 *>(ws + pl.records);
         g.grouped = reinterpret_cast<int32_t *>(ws + pl.order);
-        g.count = reinterpret_cast<int32_t *>(ws + pl.count);
+        g.counts = reinterpret_cast<int32_t *>(ws + pl.count);
+        g.slots = pl.slots;
+        g.div_slots = fast_div((uint32_t)pl.slots);
     }
     g.xs = d->x_stride;
     g.ys = d->y_stride;
