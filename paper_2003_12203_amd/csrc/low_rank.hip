@@ -46,33 +46,25 @@ struct TileTokens {
     }
 };
 
-// Calls f(adapter, its tokens) for the adapters of tile `tile`; adapter -1: tokens that have none.  By a whole wave.
-// Grouped (few tokens of a tile have different adapters then): the tile is a record.  Else a tile is neighbouring tokens, and
-// of their adapters those that fall to way `way` of `ways` are meant.
-template <int TILE, bool GROUPED, typename F>
+// Calls f(adapter, its tokens) for the adapters of tile `tile` of neighbouring tokens, of these those that fall to way `way` of
+// `ways`; adapter -1: tokens that have none.  By a whole wave.
+template <int TILE, typename F>
 __device__ __forceinline__ void each_adapter(const LowRankArgs &a, int tile, int way, int ways, F f) {
-    if constexpr (GROUPED) {
-        const int part = (int)div_by(tile, a.div_slots);
-        if (tile - part * a.slots >= a.counts[part]) return;
-        const int4 r = a.records[tile];
-        f(__builtin_amdgcn_readfirstlane(r.x), TileTokens{r.y, r.z, 0, a.grouped});
-    } else {
-        const int lane = threadIdx.x & 63, t0 = tile * TILE, count = min(TILE, a.tokens - t0);
-        int id = -1;
-        if (lane < count) {
-            id = a.ids[t0 + lane];
-            if ((unsigned)id >= (unsigned)a.adapters) id = -1;
-        }
-        unsigned long long left = __ballot(id >= 0);
-        const unsigned long long none = __ballot(lane < count && id < 0);
-        for (int k = 0; left; k = k + 1 == ways ? 0 : k + 1) {
-            const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-            const unsigned long long mine = __ballot(id == adapter);
-            left &= ~mine;
-            if (k == way) f(adapter, TileTokens{t0, count, mine, nullptr});
-        }
-        if (none && way == 0) f(-1, TileTokens{t0, count, none, nullptr});
+    const int lane = threadIdx.x & 63, t0 = tile * TILE, count = min(TILE, a.tokens - t0);
+    int id = -1;
+    if (lane < count) {
+        id = a.ids[t0 + lane];
+        if ((unsigned)id >= (unsigned)a.adapters) id = -1;
     }
+    unsigned long long left = __ballot(id >= 0);
+    const unsigned long long none = __ballot(lane < count && id < 0);
+    for (int k = 0; left; k = k + 1 == ways ? 0 : k + 1) {
+        const int adapter = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const unsigned long long mine = __ballot(id == adapter);
+        left &= ~mine;
+        if (k == way) f(adapter, TileTokens{t0, count, mine, nullptr});
+    }
+    if (none && way == 0) f(-1, TileTokens{t0, count, none, nullptr});
 }
 
 constexpr int kGroup = 1024, kPart = 2 * kGroup;   // threads of group_kernel; tokens of a workgroup of it
@@ -191,7 +183,7 @@ __global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(LowRankArgs a
     const int chunks = (a.ch + C::VALUES - 1) / C::VALUES, whole = a.ch / C::VALUES, part = split * W + w, parts = a.splits * W;
     const int blocks = max((whole / 4 - part + parts - 1) / parts, 0), groups = blocks * (4 / AHEAD);
     const auto chunk_of = [&](int g) { return (part + g / (4 / AHEAD) * parts) * 4 + g % (4 / AHEAD) * AHEAD; };
-    each_adapter<TILE, false>(a, (int)x3, way, a.ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
+    each_adapter<TILE>(a, (int)x3, way, a.ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
         if (adapter < 0) return;
         const int rank = used_rank(a, adapter);
         const T *xr[MT], *ar[NB];
@@ -419,69 +411,57 @@ __device__ __forceinline__ void narrow(uint16_t &d, float v) { d = f32_to_bf16_r
 //
 // bf16: h is the sum of two bf16 values (an error of 2^-17 of it; rounded to one, its products would be off by as
 // much as the outputs' own rounding).
-template <typename T, int MT, int RC, bool GROUPED>
-__global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
-    using C = Chunk<T>;
-    constexpr int EU = C::EU, TILE = 16 * MT, PLANES = sizeof(T) == 2 ? 2 : 1;
-    constexpr int LPR = 64 / EU, RPL = 64 / LPR, PASSES = TILE / RPL;   // lanes of a row's 64 outputs; rows of a load; loads
-    constexpr int PITCH = 68;   // floats: 16 rows begin at different banks
-    __shared__ __align__(16) float room[4][TILE * PITCH];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n16 = lane & 15, h = lane >> 4, row = lane / LPR, col = lane % LPR * EU;
-    float *mine = room[w];
-    const unsigned x1 = div_by(blockIdx.x, a.div_spans), x2 = div_by(x1, a.div_expand_ways);
-    const int way = (int)(x1 - x2 * a.expand_ways);
-    // a workgroup's waves have `together` tiles (one or four), which share the loads of B, and one or four spans of outputs
-    const long long tile = (long long)x2 * a.together + (a.together > 1 ? w : 0);
-    const long long span = a.together > 1 ? blockIdx.x - x1 * a.div_spans.d : (long long)(blockIdx.x - x1 * a.div_spans.d) * 4 + w;
-    if (tile >= a.tiles) return;
-    const int m0 = (int)min(span * a.columns, (long long)a.m), m1 = (int)min((span + 1) * a.columns, (long long)a.m);
-    if (m0 >= m1) return;
-    each_adapter<TILE, GROUPED>(a, (int)tile, way, a.expand_ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
-        if (adapter < 0) {   // no adapter: as they are
-            for (int i = 0; a.out != a.y && i < TILE; ++i) {
-                if (!tokens.has(i)) continue;
-                const long long t = tokens.token(i);
-                const T *y = static_cast<const T *>(a.y) + t * a.ys;
-                T *out = static_cast<T *>(a.out) + t * a.os;
-                for (int c = m0 + EU * lane; c < m1; c += EU * 64)
-                    *reinterpret_cast<uint4 *>(out + c) = *reinterpret_cast<const uint4 *>(y + c);
-            }
-            return;
-        }
-        const int rank = used_rank(a, adapter);
-        const T *bt = static_cast<const T *>(a.b) + adapter * a.bs[0];
-        const int steps = (m1 - m0 + 63) / 64;
-        uint4 low[MT][RC][PLANES];   // (of other tokens any values: their products go nowhere)
+__device__ __forceinline__ int output_row(int n16, int q) { return 16 * (n16 >> 2) + 4 * q + (n16 & 3); }
+
+// h of a tile's tokens, as operands: unit c * 4 + h of token 16 i + n16.  (Of tokens that are none, of others: their products go
+// nowhere.)
+template <typename T, int MT, int RC> struct Low {
+    static constexpr int EU = 16 / sizeof(T), PLANES = sizeof(T) == 2 ? 2 : 1;
+    uint4 low[MT][RC][PLANES];
+    // acc[q] += unit (c, q) of B times these
+    __device__ __forceinline__ void multiply(f32x4 (&acc)[4][MT], int c, int q, uint4 b) const {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) acc[q][t] = product<T>(b, low[t][c][p], acc[q][t]);
+    }
+    __device__ __forceinline__ void load(const LowRankArgs &a, const TileTokens &tokens) {
+        const int n16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const long long t = tokens.token(16 * i + n16);
 #pragma unroll
             for (int c = 0; c < RC; ++c) {
-                const int k = c * C::VALUES + h * EU;
+                const int k = (4 * c + h) * EU;
                 float v[EU];
 #pragma unroll
                 for (int e = 0; e < EU; ++e) v[e] = 0.0f;
                 if (k < a.rank) {
                     const float *from = a.low + t * a.rank + k;
                     const long long step = (long long)a.tokens * a.rank;
-                    for (int s = 0; s < a.splits; s += 4) {   // four ranges' loads at a time
-                        float4 f[4][EU / 4];
+                    auto add = [&](float4 f, int e) __attribute__((always_inline)) {
+                        v[e] += f.x;
+                        v[e + 1] += f.y;
+                        v[e + 2] += f.z;
+                        v[e + 3] += f.w;
+                    };
+                    if (a.splits == 1) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int e = 0; e < EU; e += 4) add(reinterpret_cast<const float4 *>(from)[e / 4], e);
+                    } else {
+                        for (int s = 0; s < a.splits; s += 4) {   // four ranges' loads at a time
+                            float4 f[4][EU / 4];
 #pragma unroll
-                            for (int e = 0; e < EU / 4; ++e)
-                                f[j][e] = reinterpret_cast<const float4 *>(from + min(s + j, a.splits - 1) * step)[e];
+                            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (s + j < a.splits)
+                                for (int e = 0; e < EU / 4; ++e)
+                                    f[j][e] = reinterpret_cast<const float4 *>(from + min(s + j, a.splits - 1) * step)[e];
 #pragma unroll
-                                for (int e = 0; e < EU; e += 4) {
-                                    v[e] += f[j][e / 4].x;
-                                    v[e + 1] += f[j][e / 4].y;
-                                    v[e + 2] += f[j][e / 4].z;
-                                    v[e + 3] += f[j][e / 4].w;
-                                }
+                            for (int j = 0; j < 4; ++j)
+                                if (s + j < a.splits)
+#pragma unroll
+                                    for (int e = 0; e < EU; e += 4) add(f[j][e / 4], e);
+                        }
                     }
                 }
                 Unit<T> hi, lo;
@@ -495,9 +475,33 @@ __global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
                 if constexpr (PLANES == 2) low[i][c][PLANES - 1] = lo.q;
             }
         }
-        bool on[PASSES];   // rows of y and the output that this lane reads and writes
-        const T *yt[PASSES];
-        T *ot[PASSES];
+    }
+};
+
+template <int MT> __device__ __forceinline__ void clear(f32x4 (&acc)[4][MT]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[q][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+
+// A wave's rows of y and the output: this lane has EU outputs, from col on, of the rows row + p RPL.
+template <typename T, int MT> struct TileRows {
+    static constexpr int EU = 16 / sizeof(T), TILE = 16 * MT, LPR = 64 / EU, RPL = 64 / LPR, PASSES = TILE / RPL;
+    static constexpr int PITCH = 68;   // floats: 16 rows begin at different banks
+    static constexpr int ROOM = TILE * PITCH;
+    struct Rows {
+        Unit<T> y[PASSES];
+    };
+    int row, col, end;
+    bool on[PASSES];
+    const T *yt[PASSES];
+    T *ot[PASSES];
+    __device__ __forceinline__ TileRows(const LowRankArgs &a, const TileTokens &tokens, int m1) {
+        const int lane = threadIdx.x & 63;
+        row = lane / LPR;
+        col = lane % LPR * EU;
+        end = m1;
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             on[p] = tokens.has(p * RPL + row);
@@ -505,103 +509,122 @@ __global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
             yt[p] = static_cast<const T *>(a.y) + t * a.ys;
             ot[p] = static_cast<T *>(a.out) + t * a.os;
         }
-        constexpr bool B_AHEAD = RC <= 2;   // (more would leave one wave to a SIMD)
-        struct Ahead {
-            uint4 b[B_AHEAD ? RC : 1][4];
-        };
-        struct Rows {
-            Unit<T> y[PASSES];
-        };
-        auto load_b = [&](uint4 (&to)[4], int c, int m) __attribute__((always_inline)) {
+    }
+    __device__ __forceinline__ void load(Rows &s, int m) const {   // of outputs m on, or the last ones
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int r = m + 16 * (n16 >> 2) + 4 * q + (n16 & 3), k = c * C::VALUES + h * EU;
-                // rows past the last: that one, for nobody; past the rank: zero, as h is
-                to[q] = *reinterpret_cast<const uint4 *>(bt + min(r, m1 - 1) * a.bs[1] + min(k, a.rank - EU));
-            }
-        };
-        // (of steps past the last: that one again, so that no load is under a condition)
-        auto load_ahead = [&](Ahead &s, int i) __attribute__((always_inline)) {
-            if constexpr (B_AHEAD) {
+        for (int p = 0; p < PASSES; ++p) s.y[p].q = *reinterpret_cast<const uint4 *>(yt[p] + min(m + col, end - EU));
+    }
+    // y and the products of outputs m on, acc[q][t] of block q and tokens 16 t.., by way of `room` in LDS, into the output
+    // (ALL: all of these rows and outputs are there; a store under a condition would make the next wait for loads one for it too)
+    template <bool ALL> __device__ __forceinline__ void store(const Rows &s, const f32x4 (&acc)[4][MT], int m, float *room) const {
+        const int n16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
 #pragma unroll
-                for (int c = 0; c < RC; ++c) load_b(s.b[c], c, m0 + 64 * min(i, steps - 1));
-            }
-        };
-        auto load_rows = [&](Rows &s, int i) __attribute__((always_inline)) {
-            const int m = min(m0 + 64 * min(i, steps - 1) + col, m1 - EU);
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) s.y[p].q = *reinterpret_cast<const uint4 *>(yt[p] + m);
-        };
-        auto multiply = [&](const Rows &s, const Ahead &ahead, int i) __attribute__((always_inline)) {
-            const int m = m0 + 64 * i;
-            f32x4 acc[4][MT];
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<f32x4 *>(room + (16 * t + n16) * PITCH + 16 * h + 4 * q) = acc[q][t];
+        // (a wave's own LDS operations are in order)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+        for (int p = 0; p < PASSES; ++p) {
+            const float *at = room + (p * RPL + row) * PITCH + col;
+            float add[EU];
 #pragma unroll
-                for (int t = 0; t < MT; ++t) acc[q][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            uint4 bf[B_AHEAD ? 1 : RC][4];
-            if constexpr (!B_AHEAD) {
+            for (int e = 0; e < EU; e += 4) *reinterpret_cast<f32x4 *>(add + e) = *reinterpret_cast<const f32x4 *>(at + e);
+            Unit<T> v;
 #pragma unroll
-                for (int c = 0; c < RC; ++c) load_b(bf[c], c, m);
-            }
-#pragma unroll
-            for (int c = 0; c < RC; ++c) {
-                const int k = c * C::VALUES + h * EU;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint4 b;
-                    if constexpr (B_AHEAD) b = ahead.b[c][q];
-                    else b = bf[c][q];
-                    if (rank < RC * C::VALUES) b = within_rank<T>(b, k, rank);
-#pragma unroll
-                    for (int t = 0; t < MT; ++t)
-#pragma unroll
-                        for (int p = 0; p < PLANES; ++p) acc[q][t] = product<T>(b, low[t][c][p], acc[q][t]);
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *reinterpret_cast<f32x4 *>(mine + (16 * t + n16) * PITCH + 16 * h + 4 * q) = acc[q][t];
-            // (a wave's own LDS operations are in order)
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int p = 0; p < PASSES; ++p) {
-                const float *at = mine + (p * RPL + row) * PITCH + col;
-                float add[EU];
-#pragma unroll
-                for (int e = 0; e < EU; e += 4) *reinterpret_cast<f32x4 *>(add + e) = *reinterpret_cast<const f32x4 *>(at + e);
-                Unit<T> v;
-#pragma unroll
-                for (int e = 0; e < EU; ++e) narrow(v.e[e], widen(s.y[p].e[e]) + add[e]);
-                if (on[p] && m + col < m1) *reinterpret_cast<uint4 *>(ot[p] + m + col) = v.q;
-            }
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_wave_barrier();
-        };
-        Ahead b0, b1;
-        Rows y0, y1, y2, y3;   // two steps ahead, B one
-        load_ahead(b0, 0);
-        load_rows(y0, 0);
-        load_rows(y1, 1);
-        for (int i = 0; i < steps; i += 4) {
-            auto step = [&](int j, Rows &now, Rows &later, Ahead &b, Ahead &next) __attribute__((always_inline)) {
-                load_ahead(next, i + j + 1);
-                load_rows(later, i + j + 2);
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(now, b, i + j);
-            };
-            step(0, y0, y2, b0, b1);
-            if (i + 1 >= steps) break;
-            step(1, y1, y3, b1, b0);
-            if (i + 2 >= steps) break;
-            step(2, y2, y0, b0, b1);
-            if (i + 3 >= steps) break;
-            step(3, y3, y1, b1, b0);
+            for (int e = 0; e < EU; ++e) narrow(v.e[e], widen(s.y[p].e[e]) + add[e]);
+            if (ALL || (on[p] && m + col < end)) *reinterpret_cast<uint4 *>(ot[p] + m + col) = v.q;
         }
-    });
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+    }
+};
+
+// Tokens without an adapter: as they are.  By a whole wave.
+template <typename T>
+__device__ __forceinline__ void copy_rows(const LowRankArgs &a, const TileTokens &tokens, int tile, int m0, int m1) {
+    constexpr int EU = 16 / sizeof(T);
+    if (a.out == a.y) return;
+    for (int i = 0; i < tile; ++i) {
+        if (!tokens.has(i)) continue;
+        const long long t = tokens.token(i);
+        const T *y = static_cast<const T *>(a.y) + t * a.ys;
+        T *out = static_cast<T *>(a.out) + t * a.os;
+        for (int c = m0 + EU * (threadIdx.x & 63); c < m1; c += EU * 64)
+            *reinterpret_cast<uint4 *>(out + c) = *reinterpret_cast<const uint4 *>(y + c);
+    }
+}
+
+// Every wave for itself: grouped, a workgroup's have four tiles of a span of outputs, whose B they find in the first-level cache
+// (in LDS, with a barrier for every 64 outputs, it took 34 us where this takes 30: 8192 tokens, 4096 outputs, rank 16, bf16; rank 64 the same);
+// else four spans of a tile.
+template <typename T, int MT, int RC, bool GROUPED>
+__global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
+    using C = Chunk<T>;
+    using Tile = TileRows<T, MT>;
+    using Rows = typename Tile::Rows;
+    constexpr int EU = C::EU, TILE = 16 * MT;
+    __shared__ __align__(16) float room[4][Tile::ROOM];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, h = lane >> 4;
+    const unsigned x1 = div_by(blockIdx.x, a.div_spans), x2 = div_by(x1, a.div_expand_ways);
+    const long long at = blockIdx.x - x1 * a.div_spans.d, span = GROUPED ? at : 4 * at + w;
+    const int m0 = (int)min(span * a.columns, (long long)a.m), m1 = (int)min((span + 1) * a.columns, (long long)a.m);
+    if (m0 >= m1) return;
+    auto tile_of = [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
+        if (adapter < 0) return copy_rows<T>(a, tokens, TILE, m0, m1);
+        const int rank = used_rank(a, adapter), steps = (m1 - m0 + 63) / 64;
+        const T *bt = static_cast<const T *>(a.b) + adapter * a.bs[0];
+        const Tile rows(a, tokens, m1);
+        typedef uint4 Operand[RC][4];
+        // (loads are of steps past the last, too, of that one again, so that none is under a condition)
+        auto load_b = [&](Operand &to, int i) __attribute__((always_inline)) {
+            const int m = m0 + 64 * min(i, steps - 1);
+#pragma unroll
+            for (int c = 0; c < RC; ++c)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)   // rows past the last: that one, for nobody; past the rank: cleared below, as h is
+                    to[c][q] = *reinterpret_cast<const uint4 *>(bt + min(m + output_row(n16, q), m1 - 1) * a.bs[1] +
+                                                                min((4 * c + h) * EU, a.rank - EU));
+        };
+        Low<T, MT, RC> low;
+        Operand b0, b1;
+        Rows y0, y1;
+        rows.load(y0, m0);
+        load_b(b0, 0);
+        low.load(a, tokens);
+        auto go = [&](auto all) __attribute__((always_inline)) {
+            auto step = [&](int i, const Operand &b, Operand &next, const Rows &now, Rows &later) __attribute__((always_inline)) {
+                load_b(next, i + 1);
+                rows.load(later, m0 + 64 * min(i + 1, steps - 1));
+                __builtin_amdgcn_sched_barrier(0);
+                f32x4 acc[4][MT];
+                clear(acc);
+#pragma unroll
+                for (int c = 0; c < RC; ++c)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        low.multiply(acc, c, q, rank < RC * C::VALUES ? within_rank<T>(b[c][q], (4 * c + h) * EU, rank) : b[c][q]);
+                rows.template store<decltype(all)::value>(now, acc, m0 + 64 * i, room[w]);
+            };
+            for (int i = 0; i < steps; i += 2) {
+                step(i, b0, b1, y0, y1);
+                if (i + 1 >= steps) break;
+                step(i + 1, b1, b0, y1, y0);
+            }
+        };
+        if (GROUPED && tokens.count == TILE && (m1 - m0) % 64 == 0) go(std::true_type{});
+        else go(std::false_type{});
+    };
+    if constexpr (GROUPED) {
+        const int tile = 4 * (int)x2 + w, part = (int)div_by(tile, a.div_slots);
+        if (tile - part * a.slots >= a.counts[part]) return;
+        const int4 r = a.records[tile];
+        tile_of(uniform(r.x), TileTokens{uniform(r.y), uniform(r.z), 0, a.grouped});
+    } else {
+        each_adapter<TILE>(a, (int)x2, (int)(x1 - x2 * a.expand_ways), a.expand_ways, tile_of);
+    }
 }
 
 template <typename T, int MT, int NB, bool GROUPED> hipError_t shrink_go(const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
@@ -624,12 +647,17 @@ template <typename T, int MT, bool GROUPED> hipError_t go(const LowRankPlan &pl,
                                             : shrink_go<T, MT, 8, GROUPED>(pl, a, st);
     if (err != hipSuccess) return err;
     const unsigned blocks = (unsigned)((pl.tiles + pl.together - 1) / pl.together) * pl.expand_ways * pl.spans;
+    auto expand = [&](auto chunks) {
+        constexpr int RC = decltype(chunks)::value;
+        expand_kernel<T, MT, RC, GROUPED><<<blocks, 256, 0, st>>>(a);
+        return hipGetLastError();
+    };
     constexpr int V = Chunk<T>::VALUES;
-    if (a.rank <= V) expand_kernel<T, MT, 1, GROUPED><<<blocks, 256, 0, st>>>(a);
-    else if (a.rank <= 2 * V) expand_kernel<T, MT, 2, GROUPED><<<blocks, 256, 0, st>>>(a);
-    else if (a.rank <= 4 * V) expand_kernel<T, MT, 4, GROUPED><<<blocks, 256, 0, st>>>(a);
-    else if constexpr (sizeof(T) == 4) expand_kernel<T, MT, 8, GROUPED><<<blocks, 256, 0, st>>>(a);
-    return hipGetLastError();
+    if (a.rank <= V) return expand(std::integral_constant<int, 1>{});
+    if (a.rank <= 2 * V) return expand(std::integral_constant<int, 2>{});
+    if (sizeof(T) == 2 || a.rank <= 4 * V) return expand(std::integral_constant<int, 4>{});
+    if constexpr (sizeof(T) == 4) return expand(std::integral_constant<int, 8>{});
+    return hipErrorInvalidValue;   // (no rank is so large)
 }
 template <typename T> hipError_t pick(const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
     if (pl.grouped) return pl.tile == 16 ? go<T, 1, true>(pl, a, st) : go<T, 2, true>(pl, a, st);
@@ -668,7 +696,7 @@ LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d) {
     p.splits = (int)std::max(1LL, std::min(chunks / (4 * kShrinkWaves), (p.grouped ? 1LL : 2LL) * kComputeUnits / ((long long)p.tiles * p.groups * p.ways)));
     // The second launch: as many spans of 64 outputs as fill two workgroups to a compute unit, and no second round of them.
     const long long blocks = (d.m + 63) / 64;
-    p.together = p.grouped || p.tiles >= 64 ? 4 : 1;
+    p.together = p.grouped ? 4 : 1;
     p.expand_ways = share(2 * kComputeUnits, p.tiles);
     const long long rows_of = (p.tiles + p.together - 1) / p.together * (long long)p.expand_ways, wide = 4 / p.together;
     const long long spans = std::max(1LL, std::min((blocks + wide - 1) / wide, 2 * kComputeUnits / rows_of));
