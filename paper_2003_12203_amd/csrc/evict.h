@@ -5,6 +5,13 @@
 
 namespace ftcnn {
 
+// Long sequences are chosen from in parts of so many places, and a part finds for those after it:
+constexpr int kEvictPart = 16384, kEvictBins = 2048;
+struct EvictPart {
+    uint32_t bins[4][kEvictBins];   // counts of bits: of the first pass, the second, the third; the first of those kept for their positions
+    uint32_t kept, holes, late;     // kept for their positions; moves' places below k and rows from k on
+};
+
 struct EvictArgs {
     void *k, *v;
     unsigned kb[3], vb[3];        // bytes: page, row, head
@@ -17,6 +24,8 @@ struct EvictArgs {
     int units;                    // 16-byte units of a row of a head
     int32_t *counts, *from, *to;  // workspace: moves of each sequence, [batch] and [batch][half]
     long long half;
+    int parts;                    // of a sequence, or 0: a workgroup's each
+    EvictPart *part;              // workspace [batch][parts]
     int shares;                   // workgroups that share a sequence's moves
     FastDiv div_page;
 };

@@ -120,17 +120,26 @@ int check_evict(const ftcnn_evict_desc *d) {
 }
 
 struct EvictRoom {
-    size_t from, to, bytes;   // after the moves' counts
-    long long half;           // moves of a sequence, at most
+    size_t from, to, part, bytes;   // after the moves' counts
+    long long half;                 // moves of a sequence, at most
+    int parts;
 };
+long long evict_longest(const ftcnn_evict_desc &d) {
+    const long long capacity = (long long)d.list_len * d.page;
+    return std::min(d.max_kv > 0 ? d.max_kv : capacity, capacity);
+}
 EvictRoom evict_room(const ftcnn_evict_desc &d) {
     EvictRoom r{};
     if (d.batch == 0) return r;
-    r.half = std::max(1LL, (long long)d.list_len * d.page / 2);
+    const long long capacity = (long long)d.list_len * d.page;
+    r.half = std::max(1LL, capacity / 2);
     const size_t list = up256((size_t)d.batch * r.half * sizeof(int32_t));
     r.from = up256((size_t)d.batch * sizeof(int32_t));
     r.to = r.from + list;
-    r.bytes = r.to + list;
+    r.part = r.to + list;
+    const long long parts = (capacity + kEvictPart - 1) / kEvictPart;
+    if (evict_longest(d) > kEvictPart && d.batch * parts * 1024 <= kMaxThreads) r.parts = (int)parts;
+    r.bytes = r.part + (size_t)d.batch * r.parts * sizeof(EvictPart);
     return r;
 }
 
@@ -385,9 +394,11 @@ int ftcnn_evict(const ftcnn_evict_desc *d, void *k_cache, void *v_cache, const i
     e.from = reinterpret_cast<int32_t *>(ws + room.from);
     e.to = reinterpret_cast<int32_t *>(ws + room.to);
     e.half = room.half;
+    e.parts = room.parts;
+    e.part = reinterpret_cast<EvictPart *>(ws + room.part);
     e.div_page = fast_div((uint32_t)d->page);
     // workgroups of a sequence: four rows of its moves each at a time, 2048 in all
-    const long long longest = std::min(d->max_kv > 0 ? d->max_kv : capacity, capacity);
+    const long long longest = evict_longest(*d);
     const long long together = std::max(1LL, (long long)kThreads / (2LL * d->kv_heads * e.units));
     e.shares = (int)std::max(1LL, std::min((longest / 2 + 4 * together - 1) / (4 * together), 2048LL / d->batch));
     FT_REQUESTS_HIP(launch_evict(e, stream), what);

@@ -96,6 +96,35 @@ def test_long_sequences(n, k, kind):
     check(s, 3, torch.tensor([n - 100, 45], dtype=torch.int32, device="cuda"), max_kv=n)
 
 
+LONG = [20000, 0, 16384, 40000, 9, 33000, 32768, 17000]
+
+
+@pytest.mark.parametrize("kind", ["heavy", "ties", "equal", "odd", "near"])
+@pytest.mark.parametrize("first,recent", [(0, 0), (3, 90), (0, 38000)])
+def test_long_and_short_together(first, recent, kind):
+    """Sequences of several parts beside shorter ones; all, some or none of what stays is kept for its position."""
+    s = make(12, LONG, [16385, 4, 16383, 30000, 3, 33000, 1, 0], kv=1, dim=8, page=48, kind=kind, positions=recent == 90)
+    check(s, first, (s["lens"] - recent).int() if recent else None)
+
+
+def test_long_in_place_and_graph():
+    spec = dict(length=[40000, 20000], keep=[9000, 19990], kv=1, dim=8, page=64, positions=True)
+    t = make(13, **spec)
+    graph = torch.cuda.CUDAGraph()
+    held = dict(lens_out=t["lens"], mass_out=t["mass"], positions_out=t["positions"])
+    room = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")   # (larger than the call asks for)
+    with torch.cuda.graph(graph):
+        run(t, first=2, workspace=room, **held)
+    for seed in range(3):
+        new = make(40 + seed, **spec)
+        for k in ("k", "v", "lists", "lens", "keep", "mass", "positions"):
+            t[k].copy_(new[k])
+        graph.replay()
+        want = check(new, 2)
+        assert all(torch.equal(a, b) for a, b in zip((t["lens"], t["mass"], t["positions"]), want))
+        assert torch.equal(new["k"], t["k"]) and torch.equal(new["v"], t["v"])
+
+
 @pytest.mark.parametrize("kv,dim,dtype", [(1, 8, "bf16"), (1, 8, "f32"), (3, 72, "bf16"), (8, 128, "bf16"), (12, 256, "f32"), (40, 40, "bf16")])
 def test_rows_of_any_size(kv, dim, dtype):
     for order in ("heads", "rows"):
