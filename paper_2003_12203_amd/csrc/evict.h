@@ -5,11 +5,14 @@
 
 namespace ftcnn {
 
-// Long sequences are chosen from in parts of so many places, and a part finds for those after it:
-constexpr int kEvictPart = 16384, kEvictBins = 2048;
-struct EvictPart {
+constexpr int kEvictHeld = 16384;   // places that a workgroup keeps, at most
+// Longer sequences are chosen from in parts of so many places, and a part finds for the others:
+constexpr int kEvictPart = 8192, kEvictBins = 2048, kEvictWaves = 16;
+struct alignas(16) EvictPart {
     uint32_t bins[4][kEvictBins];   // counts of bits: of the first pass, the second, the third; the first of those kept for their positions
+    uint4 found[3];                 // of the first part: the limit after each pass
     uint32_t kept, holes, late;     // kept for their positions; moves' places below k and rows from k on
+    uint32_t hole_at[kEvictWaves], late_at[kEvictWaves], rank[kEvictWaves];   // of the waves, in the part; of ties in all
 };
 
 struct EvictArgs {
@@ -26,6 +29,7 @@ struct EvictArgs {
     long long half;
     int parts;                    // of a sequence, or 0: a workgroup's each
     EvictPart *part;              // workspace [batch][parts]
+    int held;                     // places of a workgroup whose weights and positions it keeps in LDS
     int shares;                   // workgroups that share a sequence's moves
     FastDiv div_page;
 };

@@ -3,11 +3,17 @@
 // that stays, so that no more rows move than have to, and none that a move reads is written by another.
 //
 // Which stay: the k-th largest weight comes from counts of the bits of the weights' images as ordered integers, 11, 11 and 10
-// at a time; ties go to the lower places, by counts of the waves' votes.  Each wave has a run of neighbouring places, so that
-// places in order are waves in order.  select_kernel: a workgroup a sequence, which holds up to 16384 weights in registers.
-// part_kernel: the same in five launches, for long sequences, a workgroup for every 16384 places: three that count bits (each
-// adds up what those before counted in all parts), one that counts what each part moves, one that writes.
-// move_kernel: the moves' rows of all heads, keys and values, 16 bytes a lane.
+// at a time, until a whole bin stays; ties go to the lower places, by counts of the waves' votes.  Each wave has a run of
+// neighbouring places, so that places in order are waves in order.  What bounds it is the chain of passes and their barriers,
+// with next to no work: loops over places in LDS are short code (held in registers they were straight code, 16 us for 64
+// sequences of 4097 against 12 now), without branches, and sums over lanes and waves go through DPP.
+//
+// select_kernel: a workgroup a sequence, which keeps up to 16384 places in LDS.  64 sequences of 4097 rows, one out: 11.8 us.
+// part_kernel: five launches for longer ones, a workgroup for every 8192 places: three count bits, each with the limit from
+// the counts of the one before in all parts, one counts what moves, one writes.  131072 rows halved: 36 us (49 in parts of
+// 16384, 36 in parts of 4096; of 64 sequences of 32768 46, 52 in parts of 4096).
+// move_kernel: the moves' rows of all heads, keys and values, 16 bytes a lane, four moves on their way.  The same 131072 rows:
+// 62 us, 4.3 TB/s read and written.
 #include <algorithm>
 
 #include "evict.h"
@@ -16,8 +22,7 @@ namespace ftcnn {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-constexpr int kSelect = 1024, kWaves = kSelect / 64;
-constexpr int kHeld = kEvictPart / kSelect;     // weights that a lane keeps in registers
+constexpr int kWaves = kEvictWaves, kSelect = 64 * kWaves;
 constexpr int kBins = kEvictBins, kPasses = 3;
 
 // Bits of pass p: 31-21, 20-10, 9-0.
@@ -29,6 +34,21 @@ __device__ __forceinline__ uint32_t ordered(float w) {
     if (w != w) return 0;
     const uint32_t u = w == 0.0f ? 0u : __float_as_uint(w);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// The sum over the lanes up to this one, of 16 or 64.
+template <int LANES> __device__ __forceinline__ uint32_t scan(uint32_t x) {
+#define FT_SCAN(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false)
+    FT_SCAN(0x111, 0xf);   // row_shr 1, 2, 4, 8
+    FT_SCAN(0x112, 0xf);
+    FT_SCAN(0x114, 0xf);
+    FT_SCAN(0x118, 0xf);
+    if (LANES == 64) {
+        FT_SCAN(0x142, 0xa);   // the last of rows 0 and 2 to rows 1 and 3, of row 1 to rows 2 and 3
+        FT_SCAN(0x143, 0xc);
+    }
+#undef FT_SCAN
+    return x;
 }
 
 // A sequence as the call has it.
@@ -51,15 +71,13 @@ struct EvictSeq {
         positions_out = a.positions_out + b * a.pos;
     }
     __device__ __forceinline__ int position(int j) const { return positions ? positions[j] : j; }
-    __device__ __forceinline__ bool held(int j) const {   // kept for its position
-        const int p = position(j);
-        return p < first || (!no_since && p >= since);
-    }
+    __device__ __forceinline__ bool held_at(int p) const { return (p < first) | (!no_since & (p >= since)); }   // kept for its position
     // what stays where it is
-    __device__ __forceinline__ void keep(int j) const {
-        if (mass != mass_out) mass_out[j] = mass[j];
-        if (positions != positions_out) positions_out[j] = position(j);
+    __device__ __forceinline__ void keep(int j, float m, int p) const {
+        if (mass != mass_out) mass_out[j] = m;
+        if (positions != positions_out) positions_out[j] = p;
     }
+    __device__ __forceinline__ void keep(int j) const { keep(j, mass[j], position(j)); }
     __device__ __forceinline__ void move(int to, int from) const {   // (the outputs may be the inputs)
         mass_out[to] = mass[from];
         positions_out[to] = position(from);
@@ -71,47 +89,55 @@ struct EvictSeq {
     }
 };
 
-// The places [p0, p1) of a sequence in a workgroup: this wave's from `base` on, 64 together, run of them; the first kHeld of a
-// lane's in registers.
+// The places [p0, p1) of a sequence in a workgroup: this wave's from `base` on, 64 together, `run` of them.  The weights and
+// positions of the first of them stay in LDS, each lane's for itself; what there are more, where a sequence is longer than its
+// caller said, is read again.  (In registers the loops are straight code, which takes longer to fetch than to run.)
 struct Places {
-    int base, run, end;
-    uint32_t key[kHeld], flags;   // bit i: kept for its position
-    __device__ __forceinline__ Places(const EvictSeq &s, int p0, int p1) {
+    const float *mass;
+    const int32_t *pos;
+    int base, run, near, end;
+    uint32_t flags = 0;   // bit i of the near ones: kept for its position
+    __device__ __forceinline__ Places(const EvictSeq &s, int p0, int p1, float *room, int held) {
+        constexpr int AHEAD = 8;
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         run = (p1 - p0 + kSelect - 1) / kSelect;
+        near = min(run, held / kSelect);
         base = p0 + w * run * 64;
         end = p1;
-        float m[kHeld];
-        int p[kHeld];
+        float *m_at = room + w * (held / kWaves) + lane;
+        int32_t *p_at = reinterpret_cast<int32_t *>(m_at + held);
+        mass = m_at;
+        pos = p_at;
+        for (int i = 0; i < near; i += AHEAD) {   // (of places past the last: that one's, for nobody)
+            float m[AHEAD];
+            int p[AHEAD];
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {   // (of places past the last: that one's, for nobody)
-            if (i >= run) break;
-            const int j = min(base + 64 * i + lane, p1 - 1);
-            m[i] = s.mass[j];
-            p[i] = s.position(j);
-        }
-        flags = 0;
+            for (int q = 0; q < AHEAD; ++q) {
+                const int j = min(base + 64 * (i + q) + lane, p1 - 1);
+                m[q] = s.mass[j];
+                p[q] = j;
+            }
+            if (s.positions) {
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            key[i] = 0;
-            if (i >= run) continue;
-            key[i] = ordered(m[i]);
-            flags |= (uint32_t)(p[i] < s.first || (!s.no_since && p[i] >= s.since)) << i;
+                for (int q = 0; q < AHEAD; ++q) p[q] = s.positions[p[q]];
+            }
+#pragma unroll
+            for (int q = 0; q < AHEAD; ++q) {
+                if (i + q >= near) break;
+                m_at[64 * (i + q)] = m[q];
+                if (s.positions) p_at[64 * (i + q)] = p[q];
+                flags |= (uint32_t)s.held_at(p[q]) << (i + q);
+            }
         }
     }
-    // f(place, whether it is there, its integer, whether it is kept for its position), all lanes together
+    // f(place, whether it is there, its integer, whether it is kept for its position, its index of the near ones or -1), all
+    // lanes together
     template <typename F> __device__ __forceinline__ void each(const EvictSeq &s, F f) const {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (i < run) {
-                const int j = base + 64 * i + lane;
-                f(j, j < end, key[i], (flags >> i & 1) != 0);
-            }
-        for (int i = kHeld; i < run; ++i) {
-            const int j = base + 64 * i + lane;
-            const bool in = j < end;
-            f(j, in, in ? ordered(s.mass[j]) : 0u, in && s.held(j));
+        int j = base + (threadIdx.x & 63);
+        for (int i = 0; i < near; ++i, j += 64) f(j, j < end, ordered(mass[64 * i]), (flags >> i & 1) != 0, i);
+        for (int i = near; i < run; ++i, j += 64) {
+            const int at = min(j, end - 1);
+            f(j, j < end, ordered(s.mass[at]), s.held_at(s.position(at)), -1);
         }
     }
 };
@@ -126,43 +152,30 @@ struct Limit {
         of_held = kept > k;
         need = of_held ? k : k - kept;
         equal = need ? 0xffffffffu : 0;
+        if (need == 0) limit = 0xffffffffu;   // none is at it or over it
     }
-    __device__ __forceinline__ bool tie(bool in, uint32_t x, bool held) const {
-        return in && held == of_held && need > 0 && (x & mask) == limit;
-    }
-    // rank: of a tie among all
-    __device__ __forceinline__ bool stays(bool in, uint32_t x, bool held, bool tie, uint32_t rank) const {
-        if (!in || held != of_held) return in && held;
-        return need > 0 && ((x & mask) > limit || (tie && rank < need));
-    }
+    __device__ __forceinline__ bool candidate(bool in, bool held) const { return in & (held == of_held); }
+    __device__ __forceinline__ bool tie(bool in, uint32_t x, bool held) const { return candidate(in, held) & ((x & mask) == limit); }
+    __device__ __forceinline__ bool open() const { return need < equal; }   // some of the equal ones stay, and some go
 };
 
 // The sum over the workgroup's waves of what each has; before: of the waves before this one.
 __device__ __forceinline__ uint32_t sum_waves(uint32_t mine, uint32_t *room, uint32_t &before) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (lane == 0) room[w] = mine;
     __syncthreads();
-    uint32_t sum = 0;
-    before = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        if (i == w) before = sum;
-        sum += room[i];
-    }
-    return sum;
+    const uint32_t sums = scan<16>(room[lane % kWaves]);
+    before = w ? __builtin_amdgcn_readlane(sums, w - 1) : 0;
+    return __builtin_amdgcn_readlane(sums, kWaves - 1);
 }
 
 // The highest bin with `need` candidates in it and those above it, of counts c0, c1 of bins kBins - 1 - 2 tid and the one below
 // it: narrows the limit to that bin.  room: kWaves + 3 words.
 __device__ __forceinline__ void narrow(Limit &l, uint32_t c0, uint32_t c1, int pass, uint32_t *room) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    uint32_t incl = c0 + c1, before;
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) {
-        const uint32_t v = __shfl_up(incl, x);
-        if (lane >= x) incl += v;
-    }
-    sum_waves(__shfl(incl, 63), room, before);
+    const int tid = threadIdx.x;
+    uint32_t before;
+    uint32_t incl = scan<64>(c0 + c1);
+    sum_waves(__builtin_amdgcn_readlane(incl, 63), room, before);
     incl += before;
     const uint32_t below = incl - c0 - c1;
     if (below < l.need && l.need <= incl) {
@@ -182,53 +195,70 @@ __device__ __forceinline__ void narrow(Limit &l, uint32_t c0, uint32_t c1, int p
 __device__ __forceinline__ void count_bits(const EvictSeq &s, const Places &places, const Limit &l, int pass, uint32_t *bins) {
     const int at = shift_of(pass);
     const uint32_t bits = bits_of(pass);
-    places.each(s, [&](int, bool in, uint32_t x, bool held) {
-        if (in && held == l.of_held && (x & l.mask) == l.limit) atomicAdd(&bins[x >> at & bits], 1u);
+    places.each(s, [&](int, bool in, uint32_t x, bool held, int) {
+        if (l.tie(in, x, held)) atomicAdd(&bins[x >> at & bits], 1u);
     });
+}
+__device__ __forceinline__ uint32_t count_held(const EvictSeq &s, const Places &places) {
+    uint32_t mine = 0;
+    places.each(s, [&](int, bool in, uint32_t, bool held, int) { mine += __popcll(__builtin_amdgcn_ballot_w64(in & held)); });
+    return mine;
+}
+__device__ __forceinline__ uint32_t count_ties(const EvictSeq &s, const Places &places, const Limit &l) {
+    uint32_t mine = 0;
+    places.each(s, [&](int, bool in, uint32_t x, bool held, int) { mine += __popcll(__builtin_amdgcn_ballot_w64(l.tie(in, x, held))); });
+    return mine;
 }
 
-// Calls f(place, whether it is there, whether it stays) with this wave's ties ranked from `rank` on.
+// The set lanes of m below this one.
+__device__ __forceinline__ uint32_t below(unsigned long long m) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+// Calls f(place, whether it stays, whether it is there and goes, its index of the near ones or -1), this wave's ties ranked from
+// `rank` on.
 template <typename F>
 __device__ __forceinline__ void each_stay(const EvictSeq &s, const Places &places, const Limit &l, uint32_t rank, F f) {
-    const unsigned long long lower = (1ull << (threadIdx.x & 63)) - 1;
-    places.each(s, [&](int j, bool in, uint32_t x, bool held) {
-        const bool tie = l.tie(in, x, held);
-        const unsigned long long vote = __ballot(tie);
-        f(j, in, l.stays(in, x, held, tie, rank + __popcll(vote & lower)));
-        rank += __popcll(vote);
+    places.each(s, [&](int j, bool in, uint32_t x, bool held, int i) {
+        bool tie = l.tie(in, x, held);
+        const bool over = l.candidate(in, held) & ((x & l.mask) > l.limit);
+        if (l.open()) {
+            const unsigned long long vote = __builtin_amdgcn_ballot_w64(tie);
+            tie = tie & (rank + below(vote) < l.need);
+            rank += __popcll(vote);
+        }
+        const bool stays = over | tie | (in & held & !l.of_held);
+        f(j, stays, in & !stays, i);
     });
-}
-__device__ __forceinline__ uint32_t ties_of(const EvictSeq &s, const Places &places, const Limit &l) {
-    uint32_t mine = 0;
-    places.each(s, [&](int, bool in, uint32_t x, bool held) { mine += __popcll(__ballot(l.tie(in, x, held))); });
-    return mine;
 }
 // The holes below k and the rows from k on that stay, of this wave.
 __device__ __forceinline__ void count_moves(const EvictSeq &s, const Places &places, const Limit &l, uint32_t rank, uint32_t &holes,
                                             uint32_t &late) {
     holes = late = 0;
-    each_stay(s, places, l, rank, [&](int j, bool in, bool stays) {
-        holes += __popcll(__ballot(in && !stays && j < s.k));
-        late += __popcll(__ballot(stays && j >= s.k));
+    each_stay(s, places, l, rank, [&](int j, bool stays, bool goes, int) {
+        holes += __popcll(__builtin_amdgcn_ballot_w64(goes & (j < s.k)));
+        late += __popcll(__builtin_amdgcn_ballot_w64(stays & (j >= s.k)));
     });
 }
 // Writes them to the lists, from hole_at and late_at on, and to the outputs what stays where it is and what is free from k on.
 __device__ __forceinline__ void write_moves(const EvictSeq &s, const Places &places, const Limit &l, uint32_t rank, uint32_t hole_at,
                                             uint32_t late_at, int32_t *to, int32_t *from) {
-    const unsigned long long lower = (1ull << (threadIdx.x & 63)) - 1;
-    each_stay(s, places, l, rank, [&](int j, bool in, bool stays) {
-        const bool hole = in && !stays && j < s.k, moving = stays && j >= s.k;
-        const unsigned long long h = __ballot(hole), m = __ballot(moving);
-        if (hole) to[hole_at + __popcll(h & lower)] = j;
-        if (moving) from[late_at + __popcll(m & lower)] = j;
+    each_stay(s, places, l, rank, [&](int j, bool stays, bool goes, int i) {
+        const bool low = j < s.k, hole = goes & low, moving = stays & !low;
+        const unsigned long long h = __builtin_amdgcn_ballot_w64(hole), m = __builtin_amdgcn_ballot_w64(moving);
+        if (hole) to[hole_at + below(h)] = j;
+        if (moving) from[late_at + below(m)] = j;
         hole_at += __popcll(h);
         late_at += __popcll(m);
-        if (stays && j < s.k) s.keep(j);
-        if (in && !stays && j >= s.k) s.clear(j);
+        if (stays & low) {
+            if (i >= 0) s.keep(j, places.mass[64 * i], s.positions ? places.pos[64 * i] : j);
+            else s.keep(j);
+        }
+        if (goes & !low) s.clear(j);
     });
 }
 
 __global__ __launch_bounds__(kSelect) void select_kernel(EvictArgs a) {
+    extern __shared__ float held[];
     __shared__ uint32_t bins[kPasses][kBins];
     __shared__ uint32_t room[7][kWaves + 3];
     const int b = blockIdx.x, tid = threadIdx.x;
@@ -237,17 +267,16 @@ __global__ __launch_bounds__(kSelect) void select_kernel(EvictArgs a) {
     int moves = 0;
     if (k > 0 && k < n) {
         for (int i = tid; i < kPasses * kBins; i += kSelect) bins[0][i] = 0;
-        const Places places(s, 0, n);
-        uint32_t kept = 0, before;
-        places.each(s, [&](int, bool in, uint32_t, bool held) { kept += __popcll(__ballot(in && held)); });
-        Limit l(k, sum_waves(kept, room[0], before));
-        for (int pass = 0; pass < kPasses && l.need < l.equal; ++pass) {   // until the whole bin stays
+        const Places places(s, 0, n, held, a.held);
+        uint32_t before;
+        Limit l(k, sum_waves(count_held(s, places), room[0], before));
+        for (int pass = 0; pass < kPasses && l.open(); ++pass) {   // until the whole bin stays
             count_bits(s, places, l, pass, bins[pass]);
             __syncthreads();
             narrow(l, bins[pass][kBins - 1 - 2 * tid], bins[pass][kBins - 2 - 2 * tid], pass, room[1 + pass]);
         }
         uint32_t rank = 0, holes, late, hole_at, late_at;   // rank: of the next tie of this wave
-        if (l.need < l.equal) sum_waves(ties_of(s, places, l), room[4], rank);
+        if (l.open()) sum_waves(count_ties(s, places, l), room[4], rank);
         count_moves(s, places, l, rank, holes, late);
         moves = (int)sum_waves(holes, room[5], hole_at);
         sum_waves(late, room[6], late_at);
@@ -269,8 +298,16 @@ __global__ __launch_bounds__(kSelect) void select_kernel(EvictArgs a) {
     for (int j = n + tid; j < a.capacity; j += kSelect) s.clear(j);
 }
 
+// The sum of f over the first n parts, by each wave for itself.
+template <typename F> __device__ __forceinline__ uint32_t over_parts(int n, F f) {
+    uint32_t sum = 0;
+    for (int i = threadIdx.x & 63; i < n; i += 64) sum += f(i);
+    return __builtin_amdgcn_readlane(scan<64>(sum), 63);
+}
+
 // A launch of five for the parts of sequences.  0 to 2 count the bits of that pass, 3 what moves, 4 writes.
 template <int STEP> __global__ __launch_bounds__(kSelect) void part_kernel(EvictArgs a) {
+    extern __shared__ float held[];
     __shared__ uint32_t bins[STEP == 0 ? 2 : 1][kBins];
     __shared__ uint32_t room[7][kWaves + 3];
     const int b = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x % (unsigned)a.parts), tid = threadIdx.x;
@@ -291,12 +328,11 @@ template <int STEP> __global__ __launch_bounds__(kSelect) void part_kernel(Evict
     const int used = (s.n - 1) / kEvictPart + 1;
     if (STEP < kPasses)
         for (int i = tid; i < (STEP == 0 ? 2 : 1) * kBins; i += kSelect) bins[0][i] = 0;
-    const Places places(s, p0, p1);
+    const Places places(s, p0, p1, held, a.held);
     if constexpr (STEP == 0) {   // of both kinds, as it is not known yet from which one is chosen
-        uint32_t kept = 0, before;
-        places.each(s, [&](int, bool in, uint32_t, bool held) { kept += __popcll(__ballot(in && held)); });
-        kept = sum_waves(kept, room[0], before);
-        places.each(s, [&](int, bool in, uint32_t x, bool held) {
+        uint32_t before;
+        const uint32_t kept = sum_waves(count_held(s, places), room[0], before);
+        places.each(s, [&](int, bool in, uint32_t x, bool held, int) {
             if (in) atomicAdd(&bins[held ? 1 : 0][x >> shift_of(0)], 1u);
         });
         __syncthreads();
@@ -306,47 +342,64 @@ template <int STEP> __global__ __launch_bounds__(kSelect) void part_kernel(Evict
             mine.bins[kPasses][i] = bins[1][i];
         }
     } else {
-        uint32_t kept = 0;
-        for (int i = 0; i < used; ++i) kept += parts[i].kept;
-        Limit l(s.k, kept);
-        for (int pass = 0; pass < min(STEP, kPasses) && l.need < l.equal; ++pass) {
-            const int of = pass == 0 && l.of_held ? kPasses : pass;
-            uint32_t c0 = 0, c1 = 0;
-            for (int i = 0; i < used; ++i) {
-                const uint2 c = *reinterpret_cast<const uint2 *>(&parts[i].bins[of][kBins - 2 - 2 * tid]);
-                c0 += c.y;
-                c1 += c.x;
-            }
-            narrow(l, c0, c1, pass, room[1 + pass]);
+        Limit l(s.k, over_parts(used, [&](int i) { return parts[i].kept; }));
+        if (STEP > 1) {   // after the passes before the last one
+            const uint4 f = parts[0].found[STEP - 2];
+            l.limit = f.x;
+            l.mask = f.y;
+            l.need = f.z;
+            l.equal = f.w;
         }
+        if (STEP <= kPasses && l.open()) {
+            constexpr int PASS = STEP - 1;
+            const uint32_t *from = parts[0].bins[PASS == 0 && l.of_held ? kPasses : PASS] + kBins - 2 - 2 * tid;
+            uint32_t c0 = 0, c1 = 0;
+            for (int i = 0; i < used; i += 8) {
+                uint2 c[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    c[q] = *reinterpret_cast<const uint2 *>(from + (long long)min(i + q, used - 1) * (sizeof(EvictPart) / 4));
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    c0 += i + q < used ? c[q].y : 0;
+                    c1 += i + q < used ? c[q].x : 0;
+                }
+            }
+            narrow(l, c0, c1, PASS, room[1]);
+        }
+        if (STEP <= kPasses && part == 0 && tid == 0) mine.found[STEP - 1] = make_uint4(l.limit, l.mask, l.need, l.equal);
         if constexpr (STEP < kPasses) {
-            if (l.need == l.equal) return;   // no further pass is needed
+            if (!l.open()) return;   // no further pass is needed
             __syncthreads();
             count_bits(s, places, l, STEP, bins[0]);
             __syncthreads();
             for (int i = tid; i < kBins; i += kSelect) mine.bins[STEP][i] = bins[0][i];
         } else {
-            uint32_t rank = 0, holes, late, hole_at, late_at;   // rank: of the next tie of this wave
-            if (l.need < l.equal) {
-                sum_waves(ties_of(s, places, l), room[4], rank);
-                for (int i = 0; i < part; ++i) rank += parts[i].bins[kPasses - 1][l.limit & bits_of(kPasses - 1)];
-            }
-            count_moves(s, places, l, rank, holes, late);
-            const uint32_t hole_sum = sum_waves(holes, room[5], hole_at), late_sum = sum_waves(late, room[6], late_at);
+            const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
             if constexpr (STEP == 3) {
+                uint32_t rank = 0, holes, late, hole_at, late_at;   // rank: of the next tie of this wave
+                if (l.open()) {
+                    sum_waves(count_ties(s, places, l), room[4], rank);
+                    rank += over_parts(part, [&](int i) { return parts[i].bins[kPasses - 1][l.limit & bits_of(kPasses - 1)]; });
+                }
+                count_moves(s, places, l, rank, holes, late);
+                holes = sum_waves(holes, room[5], hole_at);
+                late = sum_waves(late, room[6], late_at);
                 if (tid == 0) {
-                    mine.holes = hole_sum;
-                    mine.late = late_sum;
+                    mine.holes = holes;
+                    mine.late = late;
+                }
+                if ((tid & 63) == 0) {
+                    mine.hole_at[w] = hole_at;
+                    mine.late_at[w] = late_at;
+                    mine.rank[w] = rank;
                 }
             } else {
-                uint32_t moves = 0;
-                for (int i = 0; i < used; ++i) {
-                    hole_at += i < part ? parts[i].holes : 0;
-                    late_at += i < part ? parts[i].late : 0;
-                    moves += parts[i].holes;
-                }
+                const uint32_t hole_at = mine.hole_at[w] + over_parts(part, [&](int i) { return parts[i].holes; });
+                const uint32_t late_at = mine.late_at[w] + over_parts(part, [&](int i) { return parts[i].late; });
+                const uint32_t moves = over_parts(used, [&](int i) { return parts[i].holes; });
                 if (part == 0 && tid == 0) a.counts[b] = (int)moves;
-                write_moves(s, places, l, rank, hole_at, late_at, a.to + b * a.half, a.from + b * a.half);
+                write_moves(s, places, l, mine.rank[w], hole_at, late_at, a.to + b * a.half, a.from + b * a.half);
             }
         }
     }
@@ -398,17 +451,23 @@ __global__ __launch_bounds__(kThreads) void move_kernel(EvictArgs a) {
 }  // namespace
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t st) {
+    const size_t room = (size_t)a.held * (a.positions ? 8 : 4);
+    hipError_t err = hipSuccess;
+    auto launch = [&](auto kernel, unsigned groups) {
+        if (err == hipSuccess) err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room);
+        if (err == hipSuccess) kernel<<<groups, kSelect, room, st>>>(a);
+        if (err == hipSuccess) err = hipGetLastError();
+    };
     if (a.parts) {
         const unsigned groups = (unsigned)a.batch * a.parts;
-        part_kernel<0><<<groups, kSelect, 0, st>>>(a);
-        part_kernel<1><<<groups, kSelect, 0, st>>>(a);
-        part_kernel<2><<<groups, kSelect, 0, st>>>(a);
-        part_kernel<3><<<groups, kSelect, 0, st>>>(a);
-        part_kernel<4><<<groups, kSelect, 0, st>>>(a);
+        launch(part_kernel<0>, groups);
+        launch(part_kernel<1>, groups);
+        launch(part_kernel<2>, groups);
+        launch(part_kernel<3>, groups);
+        launch(part_kernel<4>, groups);
     } else {
-        select_kernel<<<(unsigned)a.batch, kSelect, 0, st>>>(a);
+        launch(select_kernel, (unsigned)a.batch);
     }
-    const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     move_kernel<<<(unsigned)a.batch * a.shares, kThreads, 0, st>>>(a);
     return hipGetLastError();
