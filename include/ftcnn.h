@@ -545,7 +545,8 @@ typedef struct {
  * for the second product as the sum of two bf16 values, within 2^-16 of it.  Infinities and NaN of a token
  * or adapter reach only the tokens that have them.  An infinity in B comes out as itself or as NaN.
  * out may be y (with its strides); outputs that overlap inputs otherwise are undefined.  Rows start on 16
- * bytes.  The workspace holds the products A x.  The result does not depend on timing.  Two launches. */
+ * bytes.  The workspace holds the products A x and, of many tokens, which have the same adapter.  The result does
+ * not depend on timing.  Two launches, or three where tokens are grouped. */
 int ftcnn_low_rank_add(const ftcnn_low_rank_desc *desc, const void *y, const void *x, const void *a, const void *b,
                        const int32_t *ids, const float *scales, const int32_t *ranks, void *out, void *workspace,
                        hipStream_t stream);
@@ -603,7 +604,7 @@ typedef struct {
  * positions, and lens_out may be kv_lens.  Cache rows from place k on keep what they held.
  * A page that is listed twice, in one sequence or two, holds undefined values after it.  keep and kv_lens are
  * taken as at least 0, kv_lens as at most list_len * page, page numbers as in ftcnn_paged_attention.  Rows of the
- * cache start on 16 bytes; its strides are 0 to 2^29.  Two launches. */
+ * cache start on 16 bytes; its strides are 0 to 2^29.  Two launches, or six where sequences are long. */
 int ftcnn_evict(const ftcnn_evict_desc *desc, void *k_cache, void *v_cache, const int32_t *page_list, const int32_t *kv_lens,
                 const int32_t *keep, const float *mass, const int32_t *positions, const int32_t *since, int32_t *lens_out,
                 float *mass_out, int32_t *positions_out, void *workspace, hipStream_t stream);

@@ -3,8 +3,15 @@
 //   out_t = y_t + s_a B_a (A_a x_t),  a = ids[t],  A_a [rank][ch], B_a [m][rank],
 //
 // in two launches, each a matrix product with tiles of tokens: h = s A x, the channels split over a workgroup's
-// waves, into the workspace, and out = y + B h.  A tile's tokens may have any adapters: its workgroups go over the different ones, each
-// with the tokens that have it, the others' rows switched off.
+// waves, into the workspace, and out = y + B h.  A tile's tokens may have any adapters: its workgroups go over the
+// different ones, each with the tokens that have it, the others' rows switched off.  Where that reads much, a launch before
+// them groups the tokens by adapter, and a tile has one.
+//
+// Few tokens: latency bounds both launches, 3.6 and 4.3 us for one token (4096 channels, 6144 outputs, rank 16, bf16; at a
+// copy's rate its 0.3 MB take 0.07), 6.8 and 8.4 for 64 tokens of 48 adapters of rank 32 (32 MB of weights, 4.5 us if each
+// came once).  Many: x, y and the output at memory's rate.  8192 tokens of six adapters, 4096 channels and outputs, rank 64:
+// 5, 31 and 43 us, of which a copy's rate would take 40 in all; the last also asks the first-level cache for B, 0.5 MB, for
+// every tile of 32 tokens.
 #include <math.h>
 
 #include <algorithm>
@@ -672,7 +679,12 @@ constexpr int kMaxBins = 8000;
 LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d) {
     LowRankPlan p{};
     if (d.tokens == 0) return p;
-    p.grouped = d.tokens >= 512 && d.adapters > 1 && d.adapters < kMaxBins;
+    // Grouping the tokens is a launch (3.5 us) more.  It pays where tiles of 16 neighbours read much of the weights, each of them
+    // what all adapters have at most, or 16 of them: 48 MB.  128 tokens of 4096 channels and outputs in bf16, apart and grouped:
+    // 4 adapters of rank 16 (8 MB) 9.7 and 12.8 us, 32 of them (29 MB) 14 and 14, 8 of rank 64 (67 MB) 19.5 and 17; 300 tokens of
+    // those 8 (159 MB) 36 and 20.
+    const long long read = (d.tokens + 15LL) / 16 * std::min(16, d.adapters) * d.rank * ((long long)d.ch + d.m) * (d.dtype == FTCNN_F32 ? 4 : 2);
+    p.grouped = read > 48LL << 20 && d.adapters < kMaxBins;
     // two tiles of 16 together where they fill the device and adapters have as many tokens
     p.tile = d.tokens >= 32 * kComputeUnits / 2 && d.tokens / d.adapters >= 32 ? 32 : 16;
     p.tiles = (d.tokens + p.tile - 1) / p.tile;

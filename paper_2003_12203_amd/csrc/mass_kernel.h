@@ -9,9 +9,8 @@
 // mass_wide_kernel, more than 64 rows of a key head: a wave holds 64 keys of a head in registers (32 where heads are large, or
 // where there would be too few workgroups), tiles of 64 rows (fewer where heads are large) go through LDS, which the
 // workgroup's waves share, and the scores of the next 32 rows go through the matrix cores while these rows' weights are
-// made.  What bounds it with many rows is the vector unit beside the matrix cores: an argument, a power and a sum for each
-// weight (16 of 24 cycles' worth of the matrix cores' time for heads of 128, and the two overlap in part: a loop of
-// nothing else takes 334 ns for 32 rows of 64 keys, this kernel 545).  Two prompts of 8192 tokens, 32 heads of 128 over eight key heads,
+// made.  What bounds it with many rows is the vector unit beside the matrix cores: for each weight an argument, a power and a
+// sum, 16 cycles of it for every 24 that the matrix cores take for heads of 128, and the two overlap in part.  Two prompts of 8192 tokens, 32 heads of 128 over eight key heads,
 // bf16: 548 us, 1000 TFLOP/s of the 1260 that a product of 8192 x 8192 matrices reaches; as first written, with the weights after the
 // scores, places divided for each row and lanes added through LDS, which spilled registers, 760.
 // Short calls pay for a workgroup's start, 8 us from its lengths to its sums.

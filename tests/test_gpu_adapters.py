@@ -55,6 +55,36 @@ def test_against_float64(tokens, ch, m, count, rank, dtype):
     check(s, adapters.low_rank_add(**s), dtype)
 
 
+@pytest.mark.parametrize("tokens,ch,m,count", [(2100, 1000, 600, 70), (4100, 520, 264, 17)])
+@pytest.mark.parametrize("rank", [8, 24, 40, 72, 128])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tokens_grouped(tokens, ch, m, count, rank, dtype):
+    """More than one part of tokens; tiles of 16 and of 32; every count of rows and of chunks together."""
+    s = make(rank, tokens, ch, m, count, rank, dtype)
+    check(s, adapters.low_rank_add(**s), dtype)
+
+
+MANY = [(4100, 72, 80, 2, 8), (4100, 72, 80, 2, 24), (4100, 72, 80, 2, 64), (8200, 40, 40, 2, 128), (4100, 40, 40, 130, 72),
+        (4100, 64, 64, 8001, 8), (2049, 2048, 1032, 1, 48), (8200, 520, 264, 1, 16)]
+
+
+@pytest.mark.parametrize("tokens,ch,m,count,rank", MANY)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_tokens(tokens, ch, m, count, rank, dtype):
+    """Many tokens apart, with little to read; more adapters than are grouped; one adapter and many tokens."""
+    s = make(rank, tokens, ch, m, count, rank, dtype)
+    check(s, adapters.low_rank_add(**s), dtype)
+
+
+@pytest.mark.parametrize("kind", ["one", "none", "alone", "sorted"])
+def test_grouped_ids_of_any_kind(kind):
+    tokens, count = 2200, 64
+    ids = {"one": [3] * tokens, "none": [-1] * tokens, "alone": [-1] * 2100 + [5] + [64] * 99,
+           "sorted": sorted(t % 66 - 1 for t in range(tokens))}[kind]
+    s = make(11, tokens, 1024, 512, count, 16, "bf16", ids)
+    check(s, adapters.low_rank_add(**s), "bf16")
+
+
 @pytest.mark.parametrize("rank,ch,m", [(4, 4, 4), (12, 20, 36), (20, 1004, 516), (100, 12, 260)])
 def test_fp32_sizes_of_four(rank, ch, m):
     s = make(rank, 33, ch, m, 3, rank, "f32")
@@ -62,7 +92,7 @@ def test_fp32_sizes_of_four(rank, ch, m):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("tokens", [40, 400])
+@pytest.mark.parametrize("tokens", [40, 400, 9000])
 def test_ranks_and_what_lies_past_them(tokens, dtype):
     """Ranks of every kind, NaN past them, and adapters that no token has."""
     s = make(3, tokens, 200, 144, 9, 24, dtype)
@@ -78,10 +108,10 @@ def test_ranks_and_what_lies_past_them(tokens, dtype):
     check(clean, got, dtype, ranks)
 
 
-@pytest.mark.parametrize("tokens", [20, 300])
+@pytest.mark.parametrize("tokens,ch,m,count", [(20, 96, 80, 3), (300, 96, 80, 3), (2100, 1000, 600, 16), (4100, 520, 264, 17)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_values_that_are_not_finite_reach_only_their_token(tokens, dtype):
-    s = make(4, tokens, 96, 80, 3, 16, dtype)
+def test_values_that_are_not_finite_reach_only_their_token(tokens, ch, m, count, dtype):
+    s = make(4, tokens, ch, m, count, 16, dtype)
     clean = adapters.low_rank_add(**s)
     s["x"][7, 5], s["x"][11, 0] = float("nan"), float("inf")
     s["ids"][7] = s["ids"][11] = 1
@@ -103,7 +133,7 @@ def test_ids_out_of_range_are_no_adapter(dtype):
     assert torch.equal(adapters.low_rank_add(**s), s["y"])
 
 
-@pytest.mark.parametrize("tokens", [9, 270])
+@pytest.mark.parametrize("tokens", [9, 270, 25000])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_layouts(tokens, dtype):
     """Slices of packed rows, weights inside larger ones, in place, an output with rows of its own."""
@@ -120,7 +150,7 @@ def test_layouts(tokens, dtype):
     assert (wide["out"][:, :200] == 7).all() and (wide["out"][:, 296:] == 7).all()
     assert adapters.low_rank_add(y, x, a, b, s["ids"], s["scales"], out=y) is y and torch.equal(y, want)
     assert (wide["y"][:, :64] == 7).all() and (wide["y"][:, 160:] == 7).all()
-    alone = make(6, tokens, 128, 96, 1, 16, dtype)
+    alone = make(6, min(tokens, 300), 128, 96, 1, 16, dtype)
     alone["scales"] = None
     check(alone, adapters.low_rank_add(**alone), dtype)
 
@@ -140,7 +170,7 @@ def test_rows_past_32_bits():
     assert torch.equal(adapters.low_rank_add(y, x, a, b, s["ids"], s["scales"], out=y), want)
 
 
-@pytest.mark.parametrize("tokens,count", [(1, 4), (50, 20), (700, 5)])
+@pytest.mark.parametrize("tokens,count", [(1, 4), (50, 20), (700, 40), (6000, 40)])
 def test_same_bits_streams_and_graphs(tokens, count):
     s = make(8, tokens, 640, 512, count, 32, "bf16")
     want = adapters.low_rank_add(**s)
