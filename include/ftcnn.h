@@ -546,7 +546,7 @@ typedef struct {
  * or adapter reach only the tokens that have them.  An infinity in B comes out as itself or as NaN.
  * out may be y (with its strides); outputs that overlap inputs otherwise are undefined.  Rows start on 16
  * bytes.  The workspace holds the products A x and, of many tokens, which have the same adapter.  The result does
- * not depend on timing.  Two launches, or three where tokens are grouped. */
+ * not depend on timing.  One launch for few tokens, two, or three where many are grouped. */
 int ftcnn_low_rank_add(const ftcnn_low_rank_desc *desc, const void *y, const void *x, const void *a, const void *b,
                        const int32_t *ids, const float *scales, const int32_t *ranks, void *out, void *workspace,
                        hipStream_t stream);

@@ -17,6 +17,7 @@
 #include <algorithm>
 
 #include "evict.h"
+#include "paged_attn.h"
 
 namespace ftcnn {
 namespace {
@@ -453,20 +454,27 @@ __global__ __launch_bounds__(kThreads) void move_kernel(EvictArgs a) {
 hipError_t launch_evict(const EvictArgs &a, hipStream_t st) {
     const size_t room = (size_t)a.held * (a.positions ? 8 : 4);
     hipError_t err = hipSuccess;
-    auto launch = [&](auto kernel, unsigned groups) {
-        if (err == hipSuccess) err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room);
-        if (err == hipSuccess) kernel<<<groups, kSelect, room, st>>>(a);
-        if (err == hipSuccess) err = hipGetLastError();
+    auto launch = [&](auto which, unsigned groups) {   // the kernel of step `which`, or the one for whole sequences
+        if (err != hipSuccess) return;
+        constexpr int STEP = decltype(which)::value;
+        void (*kernel)(EvictArgs);
+        if constexpr (STEP < 0) kernel = select_kernel;
+        else kernel = part_kernel<STEP>;
+        static std::atomic<uint64_t> raised{0};   // devices whose limit is raised for this kernel
+        err = raise_lds_limit(reinterpret_cast<const void *>(kernel), (STEP < 0 ? kEvictHeld : kEvictPart) * 8, raised);
+        if (err != hipSuccess) return;
+        kernel<<<groups, kSelect, room, st>>>(a);
+        err = hipGetLastError();
     };
     if (a.parts) {
         const unsigned groups = (unsigned)a.batch * a.parts;
-        launch(part_kernel<0>, groups);
-        launch(part_kernel<1>, groups);
-        launch(part_kernel<2>, groups);
-        launch(part_kernel<3>, groups);
-        launch(part_kernel<4>, groups);
+        launch(std::integral_constant<int, 0>{}, groups);
+        launch(std::integral_constant<int, 1>{}, groups);
+        launch(std::integral_constant<int, 2>{}, groups);
+        launch(std::integral_constant<int, 3>{}, groups);
+        launch(std::integral_constant<int, 4>{}, groups);
     } else {
-        launch(select_kernel, (unsigned)a.batch);
+        launch(std::integral_constant<int, -1>{}, (unsigned)a.batch);
     }
     if (err != hipSuccess) return err;
     move_kernel<<<(unsigned)a.batch * a.shares, kThreads, 0, st>>>(a);

@@ -24,6 +24,7 @@ struct LowRankArgs {
     FastDiv div_groups, div_splits, div_ways, div_expand_ways, div_spans;
 };
 struct LowRankPlan {
+    bool both;                    // one launch for both products
     bool grouped;                 // tokens are grouped by adapter first
     int parts, slots;             // ... in so many parts, of so many tiles at most
     int tile;                     // tokens of a tile

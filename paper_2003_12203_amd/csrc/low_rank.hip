@@ -5,10 +5,10 @@
 // in two launches, each a matrix product with tiles of tokens: h = s A x, the channels split over a workgroup's
 // waves, into the workspace, and out = y + B h.  A tile's tokens may have any adapters: its workgroups go over the
 // different ones, each with the tokens that have it, the others' rows switched off.  Where that reads much, a launch before
-// them groups the tokens by adapter, and a tile has one.
+// them groups the tokens by adapter, and a tile has one.  Small calls have one launch for both products.
 //
-// Few tokens: latency bounds both launches, 3.6 and 4.3 us for one token (4096 channels, 6144 outputs, rank 16, bf16; at a
-// copy's rate its 0.3 MB take 0.07), 6.8 and 8.4 for 64 tokens of 48 adapters of rank 32 (32 MB of weights, 4.5 us if each
+// Few tokens: latency bounds every launch: 9 us for one token in one launch (4096 channels, 6144 outputs, rank 16, bf16; at a
+// copy's rate its 0.4 MB take 0.07), 6.8 and 8.4 for 64 tokens of 48 adapters of rank 32 (4.5 us for their bytes, if each
 // came once).  Many: x, y and the output at memory's rate.  8192 tokens of six adapters, 4096 channels and outputs, rank 64:
 // 5, 31 and 43 us, of which a copy's rate would take 40 in all; the last also asks the first-level cache for B, 0.5 MB, for
 // every tile of 32 tokens.
@@ -175,108 +175,123 @@ constexpr int kShrinkWaves = 8;
 // The products of a tile's tokens with 16 NB rows of their adapter's A.  A workgroup's waves share its channels, each keeps AHEAD
 // chunks of every row on their way while it multiplies as many, and their sums are added in LDS.  Rows of tokens that have another adapter,
 // and those past the rank, are read as ones that are there: their products go nowhere.
+template <typename T, int MT, int NB> struct Shrink {
+    static constexpr int W = kShrinkWaves, TILE = 16 * MT, RANK = 16 * NB, AHEAD = MT + NB <= 3 ? 4 : (MT + NB <= 6 ? 2 : 1);
+    static constexpr int SUMS = W * TILE * RANK;   // floats in LDS, [W][TILE][RANK]
+    // Of rows r0 on and range `split` of the channels, every wave's part into `sums`, by a whole workgroup.
+    __device__ static __forceinline__ void parts(const LowRankArgs &a, int adapter, const TileTokens &tokens, int r0, int split, float *sums);
+    __device__ static __forceinline__ float sum(const float *sums, int i) {   // of value i
+        float v = sums[i];
+#pragma unroll
+        for (int k = 1; k < W; ++k) v += sums[k * TILE * RANK + i];
+        return v;
+    }
+};
 template <typename T, int MT, int NB>
-__global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(LowRankArgs a) {
+__device__ __forceinline__ void Shrink<T, MT, NB>::parts(const LowRankArgs &a, int adapter, const TileTokens &tokens, int r0, int split,
+                                                         float *sums) {
     using C = Chunk<T>;
-    constexpr int W = kShrinkWaves, TILE = 16 * MT, RANK = 16 * NB, AHEAD = MT + NB <= 3 ? 4 : (MT + NB <= 6 ? 2 : 1);
-    extern __shared__ __align__(16) float sums[];   // [W][TILE][RANK]
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, h = lane >> 4;
-    const unsigned x1 = div_by(blockIdx.x, a.div_groups), x2 = div_by(x1, a.div_splits), x3 = div_by(x2, a.div_ways);
-    const int r0 = (int)(blockIdx.x - x1 * a.groups) * RANK, split = (int)(x1 - x2 * a.splits);
-    const int way = (int)(x2 - x3 * a.ways);
     // This wave's channels: every (splits * W)-th block of 256 bytes of a row, so that the waves, whose rows often lie a power of
     // two apart, are at different memory channels; AHEAD chunks of 64 bytes at a time, the last block perhaps in part.
-    const int chunks = (a.ch + C::VALUES - 1) / C::VALUES, whole = a.ch / C::VALUES, part = split * W + w, parts = a.splits * W;
-    const int blocks = max((whole / 4 - part + parts - 1) / parts, 0), groups = blocks * (4 / AHEAD);
-    const auto chunk_of = [&](int g) { return (part + g / (4 / AHEAD) * parts) * 4 + g % (4 / AHEAD) * AHEAD; };
-    each_adapter<TILE>(a, (int)x3, way, a.ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
-        if (adapter < 0) return;
-        const int rank = used_rank(a, adapter);
-        const T *xr[MT], *ar[NB];
+    const int chunks = (a.ch + C::VALUES - 1) / C::VALUES, whole = a.ch / C::VALUES, part = split * W + w, all = a.splits * W;
+    const int blocks = max((whole / 4 - part + all - 1) / all, 0), groups = blocks * (4 / AHEAD);
+    const auto chunk_of = [&](int g) { return (part + g / (4 / AHEAD) * all) * 4 + g % (4 / AHEAD) * AHEAD; };
+    const T *xr[MT], *ar[NB];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-            xr[i] = static_cast<const T *>(a.x) + tokens.token(16 * i + n16) * a.xs + h * C::EU;
+    for (int i = 0; i < MT; ++i)
+        xr[i] = static_cast<const T *>(a.x) + tokens.token(16 * i + n16) * a.xs + h * C::EU;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+        ar[j] = static_cast<const T *>(a.a) + adapter * a.as[0] + min(r0 + 16 * j + n16, a.rank - 1) * a.as[1] + h * C::EU;
+    f32x4 acc[MT][NB];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    struct Stage {
+        uint4 x[AHEAD][MT], a[AHEAD][NB];
+    } s0, s1;
+    auto load = [&](Stage &s, int c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int at = (c + k) * C::VALUES;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) s.x[k][i] = *reinterpret_cast<const uint4 *>(xr[i] + at);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) s.a[k][j] = *reinterpret_cast<const uint4 *>(ar[j] + at);
+        }
+    };
+    auto multiply = [&](const Stage &s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = product<T>(s.x[k][i], s.a[k][j], acc[i][j]);
+    };
+    // (no loads under conditions in the loop: the wait for one stage would be for both)
+    if (groups > 0) {
+        load(s0, chunk_of(0));
+        int g = 0;
+        for (; g + 2 < groups; g += 2) {
+            load(s1, chunk_of(g + 1));
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(s0);
+            load(s0, chunk_of(g + 2));
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(s1);
+        }
+        if (g + 1 < groups) {
+            load(s1, chunk_of(g + 1));
+            multiply(s0);
+            multiply(s1);
+        } else {
+            multiply(s0);
+        }
+    }
+    // the row's last chunks, less than a block: one for each wave of the last range
+    for (int c = whole / 4 * 4 + w; c < chunks && split == a.splits - 1; c += W) {
+        const int at = c * C::VALUES;
+        const bool on = at + h * C::EU < a.ch;
+        uint4 xf[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xf[i] = on ? *reinterpret_cast<const uint4 *>(xr[i] + at) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const uint4 af = on ? *reinterpret_cast<const uint4 *>(ar[j] + at) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[i][j] = product<T>(xf[i], af, acc[i][j]);
+        }
+    }
+    // rows 4 h + e of tokens, column n16 of the rank
+    __syncthreads();   // the adapter before this one
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j)
-            ar[j] = static_cast<const T *>(a.a) + adapter * a.as[0] + min(r0 + 16 * j + n16, a.rank - 1) * a.as[1] + h * C::EU;
-        f32x4 acc[MT][NB];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        struct Stage {
-            uint4 x[AHEAD][MT], a[AHEAD][NB];
-        } s0, s1;
-        auto load = [&](Stage &s, int c) __attribute__((always_inline)) {
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int at = (c + k) * C::VALUES;
-#pragma unroll
-                for (int i = 0; i < MT; ++i) s.x[k][i] = *reinterpret_cast<const uint4 *>(xr[i] + at);
-#pragma unroll
-                for (int j = 0; j < NB; ++j) s.a[k][j] = *reinterpret_cast<const uint4 *>(ar[j] + at);
-            }
-        };
-        auto multiply = [&](const Stage &s) __attribute__((always_inline)) {
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int j = 0; j < NB; ++j) acc[i][j] = product<T>(s.x[k][i], s.a[k][j], acc[i][j]);
-        };
-        // (no loads under conditions in the loop: the wait for one stage would be for both)
-        if (groups > 0) {
-            load(s0, chunk_of(0));
-            int g = 0;
-            for (; g + 2 < groups; g += 2) {
-                load(s1, chunk_of(g + 1));
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(s0);
-                load(s0, chunk_of(g + 2));
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(s1);
-            }
-            if (g + 1 < groups) {
-                load(s1, chunk_of(g + 1));
-                multiply(s0);
-                multiply(s1);
-            } else {
-                multiply(s0);
-            }
-        }
-        // the row's last chunks, less than a block: one for each wave of the last range
-        for (int c = whole / 4 * 4 + w; c < chunks && split == a.splits - 1; c += W) {
-            const int at = c * C::VALUES;
-            const bool on = at + h * C::EU < a.ch;
-            uint4 xf[MT];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) xf[i] = on ? *reinterpret_cast<const uint4 *>(xr[i] + at) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                const uint4 af = on ? *reinterpret_cast<const uint4 *>(ar[j] + at) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < MT; ++i) acc[i][j] = product<T>(xf[i], af, acc[i][j]);
-            }
-        }
-        // rows 4 h + e of tokens, column n16 of the rank
-        __syncthreads();   // the adapter before this one
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sums[(w * TILE + 16 * i + 4 * h + e) * RANK + 16 * j + n16] = acc[i][j][e];
-        __syncthreads();
+            for (int e = 0; e < 4; ++e) sums[(w * TILE + 16 * i + 4 * h + e) * RANK + 16 * j + n16] = acc[i][j][e];
+    __syncthreads();
+}
+
+template <typename T, int MT, int NB>
+__global__ __launch_bounds__(64 * kShrinkWaves) void shrink_kernel(LowRankArgs a) {
+    using S = Shrink<T, MT, NB>;
+    extern __shared__ __align__(16) float sums[];
+    const unsigned x1 = div_by(blockIdx.x, a.div_groups), x2 = div_by(x1, a.div_splits), x3 = div_by(x2, a.div_ways);
+    const int r0 = (int)(blockIdx.x - x1 * a.groups) * S::RANK, split = (int)(x1 - x2 * a.splits);
+    const int way = (int)(x2 - x3 * a.ways);
+    each_adapter<S::TILE>(a, (int)x3, way, a.ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
+        if (adapter < 0) return;
+        const int rank = used_rank(a, adapter);
+        S::parts(a, adapter, tokens, r0, split, sums);
         const float s = a.scales ? a.scales[adapter] : 1.0f;
-        for (int i = threadIdx.x; i < TILE * RANK; i += 64 * W) {
-            const int t = i / RANK, r = r0 + i % RANK;
+        for (int i = threadIdx.x; i < S::TILE * S::RANK; i += 64 * S::W) {
+            const int t = i / S::RANK, r = r0 + i % S::RANK;
             if (!tokens.has(t) || r >= a.rank) continue;
-            float v = sums[i];
-#pragma unroll
-            for (int k = 1; k < W; ++k) v += sums[k * TILE * RANK + i];
-            a.low[((long long)split * a.tokens + tokens.token(t)) * a.rank + r] = r < rank ? s * v : 0.0f;
+            a.low[((long long)split * a.tokens + tokens.token(t)) * a.rank + r] = r < rank ? s * S::sum(sums, i) : 0.0f;
         }
     });
 }
@@ -432,11 +447,12 @@ template <typename T, int MT, int RC> struct Low {
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) acc[q][t] = product<T>(b, low[t][c][p], acc[q][t]);
     }
-    __device__ __forceinline__ void load(const LowRankArgs &a, const TileTokens &tokens) {
+    // row(i): h of the tile's token i, of `splits` ranges of channels, tokens * rank values apart
+    template <typename F> __device__ __forceinline__ void load(const LowRankArgs &a, int splits, F row) {
         const int n16 = threadIdx.x & 15, h = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const long long t = tokens.token(16 * i + n16);
+            const float *of = row(16 * i + n16);
 #pragma unroll
             for (int c = 0; c < RC; ++c) {
                 const int k = (4 * c + h) * EU;
@@ -444,7 +460,7 @@ template <typename T, int MT, int RC> struct Low {
 #pragma unroll
                 for (int e = 0; e < EU; ++e) v[e] = 0.0f;
                 if (k < a.rank) {
-                    const float *from = a.low + t * a.rank + k;
+                    const float *from = of + k;
                     const long long step = (long long)a.tokens * a.rank;
                     auto add = [&](float4 f, int e) __attribute__((always_inline)) {
                         v[e] += f.x;
@@ -452,20 +468,20 @@ template <typename T, int MT, int RC> struct Low {
                         v[e + 2] += f.z;
                         v[e + 3] += f.w;
                     };
-                    if (a.splits == 1) {
+                    if (splits == 1) {
 #pragma unroll
                         for (int e = 0; e < EU; e += 4) add(reinterpret_cast<const float4 *>(from)[e / 4], e);
                     } else {
-                        for (int s = 0; s < a.splits; s += 4) {   // four ranges' loads at a time
+                        for (int s = 0; s < splits; s += 4) {   // four ranges' loads at a time
                             float4 f[4][EU / 4];
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
 #pragma unroll
                                 for (int e = 0; e < EU / 4; ++e)
-                                    f[j][e] = reinterpret_cast<const float4 *>(from + min(s + j, a.splits - 1) * step)[e];
+                                    f[j][e] = reinterpret_cast<const float4 *>(from + min(s + j, splits - 1) * step)[e];
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
-                                if (s + j < a.splits)
+                                if (s + j < splits)
 #pragma unroll
                                     for (int e = 0; e < EU; e += 4) add(f[j][e / 4], e);
                         }
@@ -563,66 +579,76 @@ __device__ __forceinline__ void copy_rows(const LowRankArgs &a, const TileTokens
     }
 }
 
+// Outputs m0 on up to m1, in `steps` of 64, of a tile's tokens with an adapter, by a wave.  load_low: h, after the first loads.
+template <typename T, int MT, int RC, bool GROUPED, typename F>
+__device__ __forceinline__ void expand_tile(const LowRankArgs &a, int adapter, const TileTokens &tokens, int m0, int m1, int steps, float *room,
+                                            F load_low) {
+    using C = Chunk<T>;
+    using Tile = TileRows<T, MT>;
+    using Rows = typename Tile::Rows;
+    constexpr int EU = C::EU, TILE = 16 * MT;
+    const int lane = threadIdx.x & 63, n16 = lane & 15, h = lane >> 4;
+    const int rank = used_rank(a, adapter);
+    const T *bt = static_cast<const T *>(a.b) + adapter * a.bs[0];
+    const Tile rows(a, tokens, m1);
+    typedef uint4 Operand[RC][4];
+    // (loads are of steps past the last, too, of that one again, so that none is under a condition)
+    auto load_b = [&](Operand &to, int i) __attribute__((always_inline)) {
+        const int m = m0 + 64 * min(i, max(steps - 1, 0));
+#pragma unroll
+        for (int c = 0; c < RC; ++c)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)   // rows past the last: that one, for nobody; past the rank: cleared below, as h is
+                to[c][q] = *reinterpret_cast<const uint4 *>(bt + min(m + output_row(n16, q), m1 - 1) * a.bs[1] +
+                                                            min((4 * c + h) * EU, a.rank - EU));
+    };
+    Low<T, MT, RC> low;
+    Operand b0, b1;
+    Rows y0, y1;
+    rows.load(y0, m0);
+    load_b(b0, 0);
+    load_low(low);
+    auto go = [&](auto all) __attribute__((always_inline)) {
+        auto step = [&](int i, const Operand &b, Operand &next, const Rows &now, Rows &later) __attribute__((always_inline)) {
+            load_b(next, i + 1);
+            rows.load(later, m0 + 64 * min(i + 1, max(steps - 1, 0)));
+            __builtin_amdgcn_sched_barrier(0);
+            f32x4 acc[4][MT];
+            clear(acc);
+#pragma unroll
+            for (int c = 0; c < RC; ++c)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    low.multiply(acc, c, q, rank < RC * C::VALUES ? within_rank<T>(b[c][q], (4 * c + h) * EU, rank) : b[c][q]);
+            rows.template store<decltype(all)::value>(now, acc, m0 + 64 * i, room);
+        };
+        for (int i = 0; i < steps; i += 2) {
+            step(i, b0, b1, y0, y1);
+            if (i + 1 >= steps) break;
+            step(i + 1, b1, b0, y1, y0);
+        }
+    };
+    if (GROUPED && tokens.count == TILE && (m1 - m0) % 64 == 0) go(std::true_type{});
+    else go(std::false_type{});
+}
+
 // Every wave for itself: grouped, a workgroup's have four tiles of a span of outputs, whose B they find in the first-level cache
 // (in LDS, with a barrier for every 64 outputs, it took 34 us where this takes 30: 8192 tokens, 4096 outputs, rank 16, bf16; rank 64 the same);
 // else four spans of a tile.
 template <typename T, int MT, int RC, bool GROUPED>
 __global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
-    using C = Chunk<T>;
-    using Tile = TileRows<T, MT>;
-    using Rows = typename Tile::Rows;
-    constexpr int EU = C::EU, TILE = 16 * MT;
-    __shared__ __align__(16) float room[4][Tile::ROOM];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n16 = lane & 15, h = lane >> 4;
+    constexpr int TILE = 16 * MT;
+    __shared__ __align__(16) float room[4][TileRows<T, MT>::ROOM];
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned x1 = div_by(blockIdx.x, a.div_spans), x2 = div_by(x1, a.div_expand_ways);
     const long long at = blockIdx.x - x1 * a.div_spans.d, span = GROUPED ? at : 4 * at + w;
     const int m0 = (int)min(span * a.columns, (long long)a.m), m1 = (int)min((span + 1) * a.columns, (long long)a.m);
     if (m0 >= m1) return;
     auto tile_of = [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
         if (adapter < 0) return copy_rows<T>(a, tokens, TILE, m0, m1);
-        const int rank = used_rank(a, adapter), steps = (m1 - m0 + 63) / 64;
-        const T *bt = static_cast<const T *>(a.b) + adapter * a.bs[0];
-        const Tile rows(a, tokens, m1);
-        typedef uint4 Operand[RC][4];
-        // (loads are of steps past the last, too, of that one again, so that none is under a condition)
-        auto load_b = [&](Operand &to, int i) __attribute__((always_inline)) {
-            const int m = m0 + 64 * min(i, steps - 1);
-#pragma unroll
-            for (int c = 0; c < RC; ++c)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)   // rows past the last: that one, for nobody; past the rank: cleared below, as h is
-                    to[c][q] = *reinterpret_cast<const uint4 *>(bt + min(m + output_row(n16, q), m1 - 1) * a.bs[1] +
-                                                                min((4 * c + h) * EU, a.rank - EU));
-        };
-        Low<T, MT, RC> low;
-        Operand b0, b1;
-        Rows y0, y1;
-        rows.load(y0, m0);
-        load_b(b0, 0);
-        low.load(a, tokens);
-        auto go = [&](auto all) __attribute__((always_inline)) {
-            auto step = [&](int i, const Operand &b, Operand &next, const Rows &now, Rows &later) __attribute__((always_inline)) {
-                load_b(next, i + 1);
-                rows.load(later, m0 + 64 * min(i + 1, steps - 1));
-                __builtin_amdgcn_sched_barrier(0);
-                f32x4 acc[4][MT];
-                clear(acc);
-#pragma unroll
-                for (int c = 0; c < RC; ++c)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        low.multiply(acc, c, q, rank < RC * C::VALUES ? within_rank<T>(b[c][q], (4 * c + h) * EU, rank) : b[c][q]);
-                rows.template store<decltype(all)::value>(now, acc, m0 + 64 * i, room[w]);
-            };
-            for (int i = 0; i < steps; i += 2) {
-                step(i, b0, b1, y0, y1);
-                if (i + 1 >= steps) break;
-                step(i + 1, b1, b0, y1, y0);
-            }
-        };
-        if (GROUPED && tokens.count == TILE && (m1 - m0) % 64 == 0) go(std::true_type{});
-        else go(std::false_type{});
+        expand_tile<T, MT, RC, GROUPED>(a, adapter, tokens, m0, m1, (m1 - m0 + 63) / 64, room[w], [&](auto &low) __attribute__((always_inline)) {
+            low.load(a, a.splits, [&](int i) { return a.low + (long long)tokens.token(i) * a.rank; });
+        });
     };
     if constexpr (GROUPED) {
         const int tile = 4 * (int)x2 + w, part = (int)div_by(tile, a.div_slots);
@@ -632,6 +658,36 @@ __global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
     } else {
         each_adapter<TILE>(a, (int)x2, (int)(x1 - x2 * a.expand_ways), a.expand_ways, tile_of);
     }
+}
+
+// Both at once, for calls so small that a launch counts: every workgroup has h of its tile's tokens for itself, in LDS, and
+// its waves have spans of outputs, the first of which are on their way meanwhile.  One token of 4096 channels and 6144 outputs,
+// rank 16, bf16: 9.0 us, the two launches 3.8 and 4.4; but a call from the host, which two launches and a workspace take
+// 13 us, takes 8.6.
+template <typename T, int NB> __global__ __launch_bounds__(64 * kShrinkWaves) void both_kernel(LowRankArgs a) {
+    using S = Shrink<T, 1, NB>;
+    constexpr int RC = (16 * NB + Chunk<T>::VALUES - 1) / Chunk<T>::VALUES, PITCH = S::RANK + 4;
+    extern __shared__ __align__(16) float sums[];   // and then the waves' rooms; then h
+    float *const low_at = sums + std::max(S::SUMS, S::W * TileRows<T, 1>::ROOM);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned x1 = div_by(blockIdx.x, a.div_spans), x2 = div_by(x1, a.div_expand_ways);
+    const long long span = (long long)S::W * (blockIdx.x - x1 * a.div_spans.d) + w;
+    const int from = (int)min(span * a.columns, (long long)a.m), m1 = (int)min((span + 1) * a.columns, (long long)a.m);
+    const int steps = (m1 - from + 63) / 64, m0 = steps ? from : 0;   // (a wave without outputs takes part in h)
+    each_adapter<16>(a, (int)x2, (int)(x1 - x2 * a.expand_ways), a.expand_ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
+        if (adapter < 0) return copy_rows<T>(a, tokens, 16, from, m1);
+        expand_tile<T, 1, RC, false>(a, adapter, tokens, m0, m1, steps, sums + w * TileRows<T, 1>::ROOM, [&](auto &low) __attribute__((always_inline)) {
+            S::parts(a, adapter, tokens, 0, 0, sums);
+            const int rank = used_rank(a, adapter);
+            const float s = a.scales ? a.scales[adapter] : 1.0f;
+            for (int i = threadIdx.x; i < 16 * S::RANK; i += 64 * S::W) {
+                const int r = i % S::RANK;
+                low_at[i / S::RANK * PITCH + r] = r < rank ? s * S::sum(sums, i) : 0.0f;
+            }
+            __syncthreads();
+            low.load(a, 1, [&](int i) { return low_at + i * PITCH; });
+        });
+    });
 }
 
 template <typename T, int MT, int NB, bool GROUPED> hipError_t shrink_go(const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
@@ -666,10 +722,31 @@ template <typename T, int MT, bool GROUPED> hipError_t go(const LowRankPlan &pl,
     if constexpr (sizeof(T) == 4) return expand(std::integral_constant<int, 8>{});
     return hipErrorInvalidValue;   // (no rank is so large)
 }
+template <typename T, int NB> hipError_t both_go(const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
+    using S = Shrink<T, 1, NB>;
+    constexpr int LDS = (std::max(S::SUMS, S::W * TileRows<T, 1>::ROOM) + 16 * (S::RANK + 4)) * (int)sizeof(float);
+    if constexpr (LDS > 65536) {
+        static std::atomic<uint64_t> raised{0};   // devices whose limit is raised for this kernel
+        const hipError_t err = raise_lds_limit(reinterpret_cast<const void *>(both_kernel<T, NB>), LDS, raised);
+        if (err != hipSuccess) return err;
+    }
+    both_kernel<T, NB><<<(unsigned)pl.tiles * pl.expand_ways * pl.spans, 64 * S::W, LDS, st>>>(a);
+    return hipGetLastError();
+}
 template <typename T> hipError_t pick(const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
+    if (pl.both) {
+        if constexpr (sizeof(T) == 2)
+            if (pl.blocks == 4) return both_go<T, 4>(pl, a, st);
+        return pl.blocks == 1 ? both_go<T, 1>(pl, a, st) : both_go<T, 2>(pl, a, st);
+    }
     if (pl.grouped) return pl.tile == 16 ? go<T, 1, true>(pl, a, st) : go<T, 2, true>(pl, a, st);
     return pl.tile == 16 ? go<T, 1, false>(pl, a, st) : go<T, 2, false>(pl, a, st);
 }
+
+// Calls of one launch: so many tokens, bytes that a workgroup reads for a tile's h, and so large a rank in bf16 (half in fp32),
+// past which registers spill.
+constexpr int kBothTokens = 64, kBothRank = 64;
+constexpr long long kBothBytes = 1 << 18;
 
 // Bins of group_kernel, two counts each, that LDS holds without more of it being asked for.
 constexpr int kMaxBins = 8000;
@@ -706,6 +783,21 @@ LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d) {
     // ranges of channels where there are too few workgroups still: four chunks of 64 bytes a wave at least
     const long long chunks = ((long long)d.ch * (d.dtype == FTCNN_F32 ? 4 : 2) + 63) / 64;
     p.splits = (int)std::max(1LL, std::min(chunks / (4 * kShrinkWaves), (p.grouped ? 1LL : 2LL) * kComputeUnits / ((long long)p.tiles * p.groups * p.ways)));
+    // One launch where every workgroup can have its tile's h for itself: 256 KB to read for it at most (16 tokens of 4096 channels,
+    // rank 16, read that: 10.3 us, in two launches 9.2, and 13 from the host).
+    const long long es = d.dtype == FTCNN_F32 ? 4 : 2;
+    p.both = !p.grouped && d.tokens <= kBothTokens && d.rank <= kBothRank * 2 / es && (d.rank + std::min(d.tokens, 16)) * (long long)d.ch * es <= kBothBytes;
+    if (p.both) {
+        const long long waves = ((d.m + 63) / 64 + kShrinkWaves - 1) / kShrinkWaves;
+        p.blocks = rows > 2 ? 4 : rows;
+        p.groups = p.splits = p.together = 1;
+        p.expand_ways = share(kComputeUnits, p.tiles);
+        const long long spans = std::max(1LL, std::min(waves, 2LL * kComputeUnits / ((long long)p.tiles * p.expand_ways)));
+        const long long each = (waves + spans - 1) / spans;
+        p.columns = (int)(64 * each);
+        p.spans = (int)((waves + each - 1) / each);
+        return p;
+    }
     // The second launch: as many spans of 64 outputs as fill two workgroups to a compute unit, and no second round of them.
     const long long blocks = (d.m + 63) / 64;
     p.together = p.grouped ? 4 : 1;

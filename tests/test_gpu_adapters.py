@@ -215,10 +215,11 @@ def test_binding_refuses():
     for k, v in bad:
         with pytest.raises(ft.FtcnnError, match="low_rank_add"):
             adapters.low_rank_add(**{**s, k: v})
-    for kw in (dict(out=s["y"][:5]), dict(out=s["y"].float()), dict(ranks=s["ids"]),
-               dict(workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))):
+    for kw in (dict(out=s["y"][:5]), dict(out=s["y"].float()), dict(ranks=s["ids"])):
         with pytest.raises(ft.FtcnnError, match="low_rank_add"):
             adapters.low_rank_add(**s, **kw)
+    with pytest.raises(ft.FtcnnError, match="low_rank_add: the workspace"):
+        adapters.low_rank_add(**make(10, 200, 64, 64, 2, 16, "bf16"), workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ft.FtcnnError, match="16 bytes"):
         adapters.low_rank_add(**{**s, "x": torch.zeros(6, 72, dtype=torch.bfloat16, device="cuda")[:, 4:68]})
     with pytest.raises(ft.FtcnnError, match="no backward"):
