@@ -85,12 +85,13 @@ class AttentionLayer:
         self.reports: List[ft.Layer] = []
         h, kv = self.heads, self.kv_heads
         qkv = self._project(x, self.w_qkv, faults[0]).view(-1, h + 2 * kv, self.dim)
-        slots = self.cache.slots(step["page_list"], step["seq"], step["positions"])
+        # (places: where a cache whose rows are no longer in the order of their positions takes the new ones)
+        slots = self.cache.slots(step["page_list"], step["seq"], step.get("places", step["positions"]))
         q, _ = paged.qk_norm_rope(qkv[:, :h], None, step["positions"], self.table, self.q_weight)
         paged.kv_append(qkv[:, h:h + kv], qkv[:, h + kv:], self.cache.k, self.cache.v, slots, step["positions"],
                         self.table, self.k_weight)
         out = paged.paged_attention(q, self.cache.k, self.cache.v, step["page_list"], step["kv_lens"],
-                                    step["q_starts"], step["max_q"], step["max_kv"])
+                                    step["q_starts"], step["max_q"], step["max_kv"], lse=step.get("lse"))
         self.qkv, self.q, self.attended = qkv, q, out
         y = self._project(out.view(-1, h * self.dim), self.w_out, faults[1])
         for layer in self.reports:   # the host's one look at a step

@@ -602,7 +602,7 @@ typedef struct {
  * same in any order, but not with a window, which goes by places.  mass_out and positions_out
  * [batch][list_len * page] move with the rows; from place k on they are 0 and -1.  They may be mass and
  * positions, and lens_out may be kv_lens.  Cache rows from place k on keep what they held.
- * A page that is listed twice, in one sequence or two, holds undefined values after it.  keep and kv_lens are
+ * A page that rows of two sequences lie in, or that a list has twice, holds undefined values after it.  keep and kv_lens are
  * taken as at least 0, kv_lens as at most list_len * page, page numbers as in ftcnn_paged_attention.  Rows of the
  * cache start on 16 bytes; its strides are 0 to 2^29.  Two launches, or six where sequences are long. */
 int ftcnn_evict(const ftcnn_evict_desc *desc, void *k_cache, void *v_cache, const int32_t *page_list, const int32_t *kv_lens,
