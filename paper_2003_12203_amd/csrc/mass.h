@@ -13,7 +13,7 @@ struct MassArgs {
     int blocks;                  // blocks of keys that the launch has for a sequence
     int head_parts, row_parts;   // workgroups that share a block's key heads, and its rows
     FastDiv div_heads, div_rows, div_blocks;   // by head_parts, row_parts, blocks
-    bool near;                   // 32 tokens of the queries lie within 2^32 bytes
+    bool near;                   // 64 rows of the queries lie within 2^32 bytes
 };
 struct MassPlan {
     int dp;                      // head size the kernel is compiled for

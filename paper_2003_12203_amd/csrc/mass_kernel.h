@@ -13,6 +13,7 @@
 // sum, 16 cycles of it for every 24 that the matrix cores take for heads of 128, and the two overlap in part.  Two prompts of 8192 tokens, 32 heads of 128 over eight key heads,
 // bf16: 548 us, 1000 TFLOP/s of the 1260 that a product of 8192 x 8192 matrices reaches; as first written, with the weights after the
 // scores, places divided for each row and lanes added through LDS, which spilled registers, 760.
+// 49 tokens over 70440 keys, 64 heads of 96 over eight: 94 us (125 with a mask in every tile that is not full).
 // Short calls pay for a workgroup's start, 8 us from its lengths to its sums.
 //
 // mass_few_kernel: the reading of the keys is all, straight into registers in the order of the matrix instructions; a
@@ -168,14 +169,27 @@ template <typename T, int DP, int KS> struct MassKeys {
 
 // The rows of a sequence that may see some keys, in tiles of ROWS.  Where the sequence has so many new tokens, a tile has
 // tokens of one query head (places in scalars); fewer are taken with their query heads one after the other.
+// How a tile's rows lie: those of one query head (by_head), or of all of the key head's, tokens' heads together, as 1 << shift of
+// them divide a tile's rows (other groups, of few tokens: shift -1).  By heads (two prompts of 8192 tokens 581 us; tokens' heads
+// together 595) unless the last tile of each, which is not full, would be another 15th.
+template <int ROWS> struct MassOrder {
+    bool by_head;
+    int shift;
+    __device__ __forceinline__ MassOrder(const AttnArgs &a, const MassSeq &sq) {
+        shift = a.group <= ROWS && (a.group & (a.group - 1)) == 0 ? __builtin_ctz(a.group) : -1;
+        const int apart = (sq.nq + ROWS - 1) / ROWS * a.group, together = (sq.nq * a.group + ROWS - 1) / ROWS;
+        by_head = sq.nq >= ROWS && (shift < 0 || apart - together <= together / 15);
+        if (by_head) shift = 0;
+    }
+};
 template <int ROWS> struct MassTiles {
     bool by_head;
     int first, last;   // tiles of a query head, or of rows
     int count;         // of all query heads
-    __device__ __forceinline__ MassTiles(const AttnArgs &a, const MassSeq &sq, int k0, int k1) {
+    __device__ __forceinline__ MassTiles(const AttnArgs &a, const MassSeq &sq, bool heads, int k0, int k1) {
         int i0, i1;
         tokens_that_see(a, sq, k0, k1, i0, i1);
-        by_head = sq.nq >= ROWS;
+        by_head = heads;
         first = by_head ? i0 / ROWS : (int)((long long)i0 * a.group / ROWS);
         last = i1 > i0 ? (by_head ? (i1 + ROWS - 1) / ROWS : (i1 * a.group + ROWS - 1) / ROWS) : first;
         count = (last - first) * (by_head ? a.group : 1);
@@ -229,29 +243,36 @@ __global__ __launch_bounds__(256, DP * sizeof(T) * KS <= 512 ? 2 : 1) void mass_
     sq.settle();
     const int32_t *list = a.page_list + (long long)b * a.list_stride;
     const int nrows = sq.nq * a.group, past = sq.kv - sq.nq, heads = a.kv_heads * a.group;
-    // this lane's loads: row row0 + i * STEP of a tile, its unit that belongs at this lane's place in LDS
+    // this lane's loads: row row0 + i * STEP of a tile, its unit that belongs at this lane's place in LDS.  Where a tile's rows are
+    // whole tokens' of all query heads, or one head's, they lie at the same distances in every tile, a tile apart.
+    const MassOrder<ROWS> order(a, sq);
+    const int shift = max(order.shift, 0), few = (1 << shift) - 1, step_tokens = ROWS >> shift;
     const int own = lane / UPR, slot = lane % UPR, row0 = w * OWN + own;
     unsigned unit[L::LOADS], place[L::LOADS];
 #pragma unroll
     for (int i = 0; i < L::LOADS; ++i) {
-        unit[i] = slot ^ L::key_unit(row0 + i * STEP);
-        place[i] = (unsigned)(row0 + i * STEP) * (unsigned)(a.qs[0] * sizeof(T)) + unit[i] * 16;
+        const int r = row0 + i * STEP;
+        unit[i] = slot ^ L::key_unit(r);
+        place[i] = (unsigned)(r >> shift) * (unsigned)(a.qs[0] * sizeof(T)) + (unsigned)(r & few) * (unsigned)(a.qs[1] * sizeof(T)) + unit[i] * 16;
     }
     const T *q0 = static_cast<const T *>(a.q) + (long long)sq.q0 * a.qs[0];
     const float *lse0 = p.lse + (long long)sq.q0 * heads;
 
     for (int kb = kb0; (long long)kb * KEYS < sq.kv; kb += p.blocks) {
         const int k0 = kb * KEYS + w * 32 * KS;   // this wave's keys
-        const MassTiles<ROWS> tiles(a, sq, kb * KEYS, min(kb * KEYS + KEYS, sq.kv));
+        const MassTiles<ROWS> tiles(a, sq, order.by_head, kb * KEYS, min(kb * KEYS + KEYS, sq.kv));
         const bool by_head = tiles.by_head;
         const int u0 = uniform(from(tiles.count, rp, p.row_parts, p.div_rows));
         const int u1 = uniform(from(tiles.count, rp + 1, p.row_parts, p.div_rows));
-        // tiles of a query head that lie within the new tokens; those of them, [whole0, whole1), whose rows see all of this
-        // wave's keys
-        const int full = by_head ? sq.nq / ROWS : 0;
-        int whole0 = 0, whole1 = k0 + 32 * KS <= sq.kv ? full : 0;
-        if (a.causal) whole0 = (max(k0 + 32 * KS - 1 - past, 0) + ROWS - 1) / ROWS;
-        if (a.window > 0) whole1 = min(whole1, max(k0 - past + a.window, 0) / ROWS);
+        // tiles that lie within the new tokens; those of them, [whole0, whole1), whose rows see all of this wave's keys (rows
+        // past the last count nowhere, their log-sums are infinite)
+        const int full = by_head ? sq.nq / ROWS : (order.shift < 0 ? 0 : nrows / ROWS), each = by_head ? 1 : a.group;
+        int whole0 = 0, whole1 = k0 + 32 * KS <= sq.kv ? (sq.nq * each + ROWS - 1) / ROWS : 0;
+        if (a.causal) whole0 = (min(max(k0 + 32 * KS - 1 - past, 0), sq.nq) * each + ROWS - 1) / ROWS;
+        if (a.window > 0) {
+            const long long seen = (long long)k0 - past + a.window;   // tokens before this one see the first key
+            if (seen < sq.nq) whole1 = min(whole1, max((int)seen, 0) * each / ROWS);
+        }
         Keys keys;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
@@ -279,8 +300,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) * KS <= 512 ? 2 : 1) void mass_
             const T *q_at;
             const float *lse_at;
             auto locate = [&]() __attribute__((always_inline)) {
-                q_at = q_head + (long long)(ROWS * coming.tile) * a.qs[0] + (long long)coming.head * a.qs[1];
-                lse_at = lse_head + (long long)(ROWS * coming.tile) * heads + coming.head;
+                q_at = q_head + (long long)(step_tokens * coming.tile) * a.qs[0] + (long long)coming.head * a.qs[1];
+                lse_at = lse_head + (long long)(step_tokens * coming.tile) * heads + coming.head;
             };
             locate();
             float log[QS], next_log[QS] = {};
@@ -290,7 +311,11 @@ __global__ __launch_bounds__(256, DP * sizeof(T) * KS <= 512 ? 2 : 1) void mass_
                     const unsigned to = lds_at + ((issued - u0) & 1) * L::SIDE + w * OWN * RB;
                     if (p.near && coming.tile < full) {
 #pragma unroll
-                        for (int i = 0; i < QS; ++i) next_log[i] = lse_at[(unsigned)(32 * i + l32) * (unsigned)heads];
+                        for (int i = 0; i < QS; ++i) {
+                            int r = 32 * i + l32;
+                            asm volatile("" : "+v"(r));   // here: its offset would not find a register across the loop
+                            next_log[i] = lse_at[(unsigned)(r >> shift) * (unsigned)heads + (r & few)];
+                        }
 #pragma unroll
                         for (int i = 0; i < L::LOADS; ++i) {
                             if (DP != a.dim && (int)unit[i] * EU >= a.dim) continue;
@@ -302,6 +327,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) * KS <= 512 ? 2 : 1) void mass_
                         for (int i = 0; i < QS; ++i) {
                             row_of(coming, 32 * i + l32, token, head);
                             next_log[i] = lse_head[(long long)token * heads + head];
+                            if (ROWS * coming.tile + 32 * i + l32 >= (by_head ? sq.nq : nrows)) next_log[i] = INFINITY;
                         }
 #pragma unroll
                         for (int i = 0; i < L::LOADS; ++i) {
@@ -316,8 +342,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) * KS <= 512 ? 2 : 1) void mass_
                 if (coming.on(tiles)) {
                     locate();
                 } else {
-                    q_at += ROWS * a.qs[0];
-                    lse_at += ROWS * heads;
+                    q_at += step_tokens * a.qs[0];
+                    lse_at += step_tokens * heads;
                 }
             };
             // The tile issued last has landed, and nobody reads the one before it any more.

@@ -326,7 +326,7 @@ int ftcnn_attention_mass(const ftcnn_mass_desc *d, const void *q, const void *k_
     m.div_heads = fast_div((uint32_t)pl.head_parts);
     m.div_rows = fast_div((uint32_t)pl.row_parts);
     m.div_blocks = fast_div((uint32_t)pl.blocks);
-    m.near = d->q_stride[0] >= 0 && d->q_stride[0] < 1 << 24;
+    m.near = d->q_stride[0] >= 0 && d->q_stride[0] < 1 << 24 && d->q_stride[1] >= 0 && d->q_stride[1] < 1 << 23;
     FT_REQUESTS_HIP(d->dtype == FTCNN_F32 ? launch_mass_f32(pl, m, stream) : launch_mass_bf16(pl, m, stream), what);
     if (pl.bytes) FT_REQUESTS_HIP(launch_mass_join(pl, m, stream), "attention_mass: join");
     return FTCNN_OK;

@@ -81,6 +81,31 @@ def test_against_float64(i, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 8, 12, 32, 64, 80])
+@pytest.mark.parametrize("window,causal", [(0, True), (250, True), (0, False)])
+def test_tiles_of_tokens_heads(group, window, causal, dtype):
+    """Tokens' heads together in tiles, or one head's rows; last tiles that are not full, before keys that all rows see."""
+    new, length = [33, 3, 129, 64, 17], [600, 700, 900, 520, 16]
+    s = make(group, dtype, new, length, group, 1, 64, 16)
+    with_lse(s, causal=causal, window=window)
+    check(s, call(s, causal=causal, window=window, max_q=129, max_kv=900), causal, window)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_last_rows_that_are_not_finite(dtype):
+    """The last token's queries, which stand in for the rows behind it, reach only the keys that it sees."""
+    s = make(63, dtype, [49, 40], [400, 300], 8, 2, 128, 16)
+    s["q"][48, 3, 5], s["q"][88, 7, 0] = float("nan"), float("inf")
+    with_lse(s)
+    got = call(s, max_q=49, max_kv=400)
+    assert got[0, :400].isnan().all() and torch.equal(got[0, 400:], s["mass"][0, 400:])
+    clean = dict(s, q=s["q"].clone())
+    clean["q"][88, 7, 0] = clean["q"][48, 3, 5] = 1.0
+    with_lse(clean)
+    assert got[1, 299].isnan() and not call(clean, max_q=49, max_kv=400).isnan().any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_hints_shape_the_launch_only(dtype):
     """Too small, too large or missing: another order of the sums, and both kernels over any count of rows."""
     s = make(50, dtype, [40, 1, 9], [400, 290, 9], 4, 2, 64, 16)
