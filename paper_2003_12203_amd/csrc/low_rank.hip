@@ -591,41 +591,50 @@ __device__ __forceinline__ void expand_tile(const LowRankArgs &a, int adapter, c
     const int rank = used_rank(a, adapter);
     const T *bt = static_cast<const T *>(a.b) + adapter * a.bs[0];
     const Tile rows(a, tokens, m1);
-    typedef uint4 Operand[RC][4];
-    // (loads are of steps past the last, too, of that one again, so that none is under a condition)
-    auto load_b = [&](Operand &to, int i) __attribute__((always_inline)) {
+    uint4 b[RC][4];
+    // block q of B of step i (of steps past the last, of that one again, so that no load is under a condition)
+    auto load_b = [&](int q, int i) __attribute__((always_inline)) {
         const int m = m0 + 64 * min(i, max(steps - 1, 0));
 #pragma unroll
-        for (int c = 0; c < RC; ++c)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)   // rows past the last: that one, for nobody; past the rank: cleared below, as h is
-                to[c][q] = *reinterpret_cast<const uint4 *>(bt + min(m + output_row(n16, q), m1 - 1) * a.bs[1] +
-                                                            min((4 * c + h) * EU, a.rank - EU));
+        for (int c = 0; c < RC; ++c)   // rows past the last: that one, for nobody; past the rank: cleared below, as h is
+            b[c][q] = *reinterpret_cast<const uint4 *>(bt + min(m + output_row(n16, q), m1 - 1) * a.bs[1] +
+                                                       min((4 * c + h) * EU, a.rank - EU));
     };
     Low<T, MT, RC> low;
-    Operand b0, b1;
     Rows y0, y1;
     rows.load(y0, m0);
-    load_b(b0, 0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) load_b(q, 0);
     load_low(low);
+    const int edge = rank / C::VALUES;   // the chunk that the rank ends in, and what of it counts
+    const uint4 inside = within_rank<T>(make_uint4(~0u, ~0u, ~0u, ~0u), (4 * edge + h) * EU, rank);
     auto go = [&](auto all) __attribute__((always_inline)) {
-        auto step = [&](int i, const Operand &b, Operand &next, const Rows &now, Rows &later) __attribute__((always_inline)) {
-            load_b(next, i + 1);
+        auto step = [&](int i, const Rows &now, Rows &later) __attribute__((always_inline)) {
             rows.load(later, m0 + 64 * min(i + 1, max(steps - 1, 0)));
-            __builtin_amdgcn_sched_barrier(0);
             f32x4 acc[4][MT];
             clear(acc);
 #pragma unroll
-            for (int c = 0; c < RC; ++c)
+            for (int q = 0; q < 4; ++q) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    low.multiply(acc, c, q, rank < RC * C::VALUES ? within_rank<T>(b[c][q], (4 * c + h) * EU, rank) : b[c][q]);
+                for (int c = 0; c < RC; ++c) {
+                    if (c >= edge) {
+                        b[c][q].x &= c == edge ? inside.x : 0;
+                        b[c][q].y &= c == edge ? inside.y : 0;
+                        b[c][q].z &= c == edge ? inside.z : 0;
+                        b[c][q].w &= c == edge ? inside.w : 0;
+                    }
+                    low.multiply(acc, c, q, b[c][q]);
+                }
+                load_b(q, i + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             rows.template store<decltype(all)::value>(now, acc, m0 + 64 * i, room);
         };
-        for (int i = 0; i < steps; i += 2) {
-            step(i, b0, b1, y0, y1);
-            if (i + 1 >= steps) break;
-            step(i + 1, b1, b0, y1, y0);
+        // (one step's code, and its copies: short calls wait for code as for data)
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i) {
+            step(i, y0, y1);
+            y0 = y1;
         }
     };
     if (GROUPED && tokens.count == TILE && (m1 - m0) % 64 == 0) go(std::true_type{});
@@ -636,7 +645,7 @@ __device__ __forceinline__ void expand_tile(const LowRankArgs &a, int adapter, c
 // (in LDS, with a barrier for every 64 outputs, it took 34 us where this takes 30: 8192 tokens, 4096 outputs, rank 16, bf16; rank 64 the same);
 // else four spans of a tile.
 template <typename T, int MT, int RC, bool GROUPED>
-__global__ __launch_bounds__(256) void expand_kernel(LowRankArgs a) {
+__global__ __launch_bounds__(256, MT * RC * (int)sizeof(T) <= 8 ? 2 : 1) void expand_kernel(LowRankArgs a) {
     constexpr int TILE = 16 * MT;
     __shared__ __align__(16) float room[4][TileRows<T, MT>::ROOM];
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
