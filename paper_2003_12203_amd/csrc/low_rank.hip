@@ -769,8 +769,8 @@ LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d) {
     // what all adapters have at most, or 16 of them: 48 MB.  128 tokens of 4096 channels and outputs in bf16, apart and grouped:
     // 4 adapters of rank 16 (8 MB) 9.7 and 12.8 us, 32 of them (29 MB) 14 and 14, 8 of rank 64 (67 MB) 19.5 and 17; 300 tokens of
     // those 8 (159 MB) 36 and 20.
-    const long long read = (d.tokens + 15LL) / 16 * std::min(16, d.adapters) * d.rank * ((long long)d.ch + d.m) * (d.dtype == FTCNN_F32 ? 4 : 2);
-    p.grouped = read > 48LL << 20 && d.adapters < kMaxBins;
+    const double read = (d.tokens + 15) / 16 * (double)std::min(16, d.adapters) * d.rank * ((double)d.ch + d.m) * (d.dtype == FTCNN_F32 ? 4 : 2);
+    p.grouped = read > 48 << 20 && d.adapters < kMaxBins;
     // two tiles of 16 together where they fill the device and adapters have as many tokens
     p.tile = d.tokens >= 32 * kComputeUnits / 2 && d.tokens / d.adapters >= 32 ? 32 : 16;
     p.tiles = (d.tokens + p.tile - 1) / p.tile;

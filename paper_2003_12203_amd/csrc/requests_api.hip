@@ -77,7 +77,8 @@ int check_low_rank(const ftcnn_low_rank_desc *d) {
     if (!whole_units(vec, d->x_stride, d->y_stride, d->out_stride, d->a_stride[0], d->a_stride[1], d->b_stride[0],
                      d->b_stride[1]))
         return set_error(FTCNN_E_UNSUPPORTED, "%s: rows of tokens and adapters must start on 16 bytes", what);
-    if (d->tokens > kMaxRows) return set_error(FTCNN_E_SHAPE, "%s: more than 2^30 tokens", what);
+    if (d->tokens > kMaxRows || d->ch > kMaxRows || d->m > kMaxRows)
+        return set_error(FTCNN_E_SHAPE, "%s: more than 2^30 tokens, channels or outputs", what);
     if (d->tokens) {
         const LowRankPlan p = low_rank_plan(*d);
         const long long one = (long long)p.tiles * p.ways * p.splits * p.groups, two = (long long)p.tiles * p.expand_ways * p.spans;

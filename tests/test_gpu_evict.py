@@ -142,6 +142,13 @@ def test_in_place_and_hints():
         assert torch.equal(s["k"], t["k"]) and torch.equal(s["v"], t["v"])
 
 
+@pytest.mark.parametrize("n,hint", [(5000, 1), (5000, 1025), (40000, 100), (17000, 16384), (9000, 40000)])
+def test_hints_that_are_wrong(n, hint):
+    """Longer sequences than the caller said, and lists for far more than there is."""
+    s = make(n, [n, 70], [n // 3, 69], kv=1, dim=8, page=64, kind="ties", positions=True, extra=300)
+    check(s, 3, torch.tensor([n - 100, 60], dtype=torch.int32, device="cuda"), max_kv=hint)
+
+
 def test_layouts():
     """Caches inside larger ones, a mass and positions with rows of their own and more places than the lists name."""
     s = make(8, [200, 100], [90, 99], kv=2, dim=32, page=16, positions=True)

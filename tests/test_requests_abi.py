@@ -66,7 +66,7 @@ def call_evict(d, k=P, v=P, lists=P, lens=P, keep=P, m=P, pos=P, since=P, lo=P, 
     (dict(rank=0), E_SHAPE), (dict(rank=-8), E_SHAPE), (dict(ch=60), E_UNSUPPORTED), (dict(m=4), E_UNSUPPORTED),
     (dict(rank=12), E_UNSUPPORTED), (dict(rank=136), E_UNSUPPORTED), (dict(x_stride=68), E_UNSUPPORTED),
     (dict(y_stride=-4), E_UNSUPPORTED), (dict(out_stride=130), E_UNSUPPORTED), ({("a_stride", 0): 1028}, E_UNSUPPORTED),
-    ({("b_stride", 1): 20}, E_UNSUPPORTED), (dict(tokens=(1 << 30) + 1), E_SHAPE),
+    ({("b_stride", 1): 20}, E_UNSUPPORTED), (dict(tokens=(1 << 30) + 1), E_SHAPE), (dict(ch=(1 << 31) - 8), E_SHAPE), (dict(m=(1 << 31) - 8), E_SHAPE),
     (dict(tokens=1 << 30, m=1 << 30, out_stride=1 << 30), E_SHAPE)])
 def test_low_rank_add_refuses(kw, code):
     d = low_rank(kw)
