@@ -437,11 +437,12 @@ def evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_list: torch.Tensor,
     if lens_out is None:
         lens_out = torch.empty_like(kv_lens)
     if mass_out is None:
-        mass_out = torch.empty((batch, capacity), dtype=_F32, device=k_cache.device)
+        mass_out = torch.empty_like(mass if mass.shape[1] == capacity else mass[:, :capacity])
     else:
         _places(what, "mass_out", mass_out, _F32, batch, capacity, dev)
     if positions_out is None:
-        positions_out = torch.empty((batch, capacity), dtype=_I32, device=k_cache.device)
+        positions_out = (torch.empty_like(mass_out, dtype=_I32) if positions is None or positions.shape[1] != capacity else
+                         torch.empty_like(positions))
     else:
         _places(what, "positions_out", positions_out, _I32, batch, capacity, dev)
     kc, vc = k_cache.stride(), v_cache.stride()
