@@ -79,9 +79,9 @@ struct EvictSeq {
         if (positions != positions_out) positions_out[j] = p;
     }
     __device__ __forceinline__ void keep(int j) const { keep(j, mass[j], position(j)); }
-    __device__ __forceinline__ void move(int to, int from) const {   // (the outputs may be the inputs)
-        mass_out[to] = mass[from];
-        positions_out[to] = position(from);
+    __device__ __forceinline__ void move(int to, int from, float m, int p) const {   // (the outputs may be the inputs)
+        mass_out[to] = m;
+        positions_out[to] = p;
         clear(from);
     }
     __device__ __forceinline__ void clear(int j) const {
@@ -105,7 +105,7 @@ struct Places {
         near = min(run, held / kSelect);
         base = p0 + w * run * 64;
         end = p1;
-        float *m_at = room + w * (held / kWaves) + lane;
+        float *m_at = room + w * near * 64 + lane;   // (all near: by places)
         int32_t *p_at = reinterpret_cast<int32_t *>(m_at + held);
         mass = m_at;
         pos = p_at;
@@ -168,6 +168,15 @@ __device__ __forceinline__ uint32_t sum_waves(uint32_t mine, uint32_t *room, uin
     const uint32_t sums = scan<16>(room[lane % kWaves]);
     before = w ? __builtin_amdgcn_readlane(sums, w - 1) : 0;
     return __builtin_amdgcn_readlane(sums, kWaves - 1);
+}
+
+// Two of them with one barrier: the sums, and `before` of each.
+__device__ __forceinline__ uint2 sum_waves(uint2 mine, uint32_t *room0, uint32_t *room1, uint2 &before) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (lane == 0) room1[w] = mine.y;
+    const uint32_t x = sum_waves(mine.x, room0, before.x), sums = scan<16>(room1[lane % kWaves]);
+    before.y = w ? __builtin_amdgcn_readlane(sums, w - 1) : 0;
+    return make_uint2(x, __builtin_amdgcn_readlane(sums, kWaves - 1));
 }
 
 // The highest bin with `need` candidates in it and those above it, of counts c0, c1 of bins kBins - 1 - 2 tid and the one below
@@ -241,13 +250,20 @@ __device__ __forceinline__ void count_moves(const EvictSeq &s, const Places &pla
     });
 }
 // Writes them to the lists, from hole_at and late_at on, and to the outputs what stays where it is and what is free from k on.
+// near: to lists in LDS as well (to, from by turns).
 __device__ __forceinline__ void write_moves(const EvictSeq &s, const Places &places, const Limit &l, uint32_t rank, uint32_t hole_at,
-                                            uint32_t late_at, int32_t *to, int32_t *from) {
+                                            uint32_t late_at, int32_t *to, int32_t *from, uint16_t *near) {
     each_stay(s, places, l, rank, [&](int j, bool stays, bool goes, int i) {
         const bool low = j < s.k, hole = goes & low, moving = stays & !low;
         const unsigned long long h = __builtin_amdgcn_ballot_w64(hole), m = __builtin_amdgcn_ballot_w64(moving);
-        if (hole) to[hole_at + below(h)] = j;
-        if (moving) from[late_at + below(m)] = j;
+        if (hole) {
+            to[hole_at + below(h)] = j;
+            if (near) near[2 * (hole_at + below(h))] = (uint16_t)j;
+        }
+        if (moving) {
+            from[late_at + below(m)] = j;
+            if (near) near[2 * (late_at + below(m)) + 1] = (uint16_t)j;
+        }
         hole_at += __popcll(h);
         late_at += __popcll(m);
         if (stays & low) {
@@ -276,22 +292,36 @@ __global__ __launch_bounds__(kSelect) void select_kernel(EvictArgs a) {
             __syncthreads();
             narrow(l, bins[pass][kBins - 1 - 2 * tid], bins[pass][kBins - 2 - 2 * tid], pass, room[1 + pass]);
         }
-        uint32_t rank = 0, holes, late, hole_at, late_at;   // rank: of the next tie of this wave
+        uint32_t rank = 0;   // of the next tie of this wave
         if (l.open()) sum_waves(count_ties(s, places, l), room[4], rank);
-        count_moves(s, places, l, rank, holes, late);
-        moves = (int)sum_waves(holes, room[5], hole_at);
-        sum_waves(late, room[6], late_at);
+        uint2 mine, at;      // holes and rows that move
+        count_moves(s, places, l, rank, mine.x, mine.y);
+        moves = (int)sum_waves(mine, room[5], room[6], at).x;
         int32_t *to = a.to + b * a.half, *from = a.from + b * a.half;
-        write_moves(s, places, l, rank, hole_at, late_at, to, from);
-        __syncthreads();
-        for (int i = tid; i < moves; i += kSelect) s.move(to[i], from[i]);
+        // the lists in LDS, where the bins were, save the way to memory and back
+        if (places.near == places.run && moves <= kPasses * kBins) {
+            uint16_t *list = reinterpret_cast<uint16_t *>(bins[0]);
+            write_moves(s, places, l, rank, at.x, at.y, to, from, list);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            tile_barrier();
+            const float *held_mass = held;
+            const int32_t *held_at = reinterpret_cast<const int32_t *>(held + a.held);
+            for (int i = tid; i < moves; i += kSelect) {
+                const int t = list[2 * i], f = list[2 * i + 1];
+                s.move(t, f, held_mass[f], s.positions ? held_at[f] : f);
+            }
+        } else {
+            write_moves(s, places, l, rank, at.x, at.y, to, from, nullptr);
+            __syncthreads();
+            for (int i = tid; i < moves; i += kSelect) s.move(to[i], from[i], s.mass[from[i]], s.position(from[i]));
+        }
     } else {
         for (int j = tid; j < n; j += kSelect) {
             if (j < k) s.keep(j);
             else s.clear(j);
         }
+        __syncthreads();   // the length, which may be written where it was, has been read
     }
-    __syncthreads();   // the length, which may be written where it was, has been read
     if (tid == 0) {
         a.lens_out[b] = k;
         a.counts[b] = moves;
@@ -378,21 +408,21 @@ template <int STEP> __global__ __launch_bounds__(kSelect) void part_kernel(Evict
         } else {
             const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
             if constexpr (STEP == 3) {
-                uint32_t rank = 0, holes, late, hole_at, late_at;   // rank: of the next tie of this wave
+                uint32_t rank = 0, holes, late;   // rank: of the next tie of this wave
                 if (l.open()) {
                     sum_waves(count_ties(s, places, l), room[4], rank);
                     rank += over_parts(part, [&](int i) { return parts[i].bins[kPasses - 1][l.limit & bits_of(kPasses - 1)]; });
                 }
                 count_moves(s, places, l, rank, holes, late);
-                holes = sum_waves(holes, room[5], hole_at);
-                late = sum_waves(late, room[6], late_at);
+                uint2 at;
+                const uint2 sums = sum_waves(make_uint2(holes, late), room[5], room[6], at);
                 if (tid == 0) {
-                    mine.holes = holes;
-                    mine.late = late;
+                    mine.holes = sums.x;
+                    mine.late = sums.y;
                 }
                 if ((tid & 63) == 0) {
-                    mine.hole_at[w] = hole_at;
-                    mine.late_at[w] = late_at;
+                    mine.hole_at[w] = at.x;
+                    mine.late_at[w] = at.y;
                     mine.rank[w] = rank;
                 }
             } else {
@@ -400,7 +430,7 @@ template <int STEP> __global__ __launch_bounds__(kSelect) void part_kernel(Evict
                 const uint32_t late_at = mine.late_at[w] + over_parts(part, [&](int i) { return parts[i].late; });
                 const uint32_t moves = over_parts(used, [&](int i) { return parts[i].holes; });
                 if (part == 0 && tid == 0) a.counts[b] = (int)moves;
-                write_moves(s, places, l, mine.rank[w], hole_at, late_at, a.to + b * a.half, a.from + b * a.half);
+                write_moves(s, places, l, mine.rank[w], hole_at, late_at, a.to + b * a.half, a.from + b * a.half, nullptr);
             }
         }
     }
@@ -412,7 +442,10 @@ __global__ __launch_bounds__(kThreads) void move_kernel(EvictArgs a) {
     const int moves = a.counts[b];
     if (a.parts) {   // the weights and positions that move, and the length, which nobody else reads here
         const EvictSeq s(a, b);
-        for (int i = share * kThreads + threadIdx.x; i < moves; i += a.shares * kThreads) s.move(a.to[b * a.half + i], a.from[b * a.half + i]);
+        for (int i = share * kThreads + threadIdx.x; i < moves; i += a.shares * kThreads) {
+            const int f = a.from[b * a.half + i];
+            s.move(a.to[b * a.half + i], f, s.mass[f], s.position(f));
+        }
         if (share == 0 && threadIdx.x == 0) a.lens_out[b] = s.k;
     }
     const int side = a.kv_heads * a.units, units = 2 * side;   // of a move
