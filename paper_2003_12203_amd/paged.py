@@ -114,8 +114,9 @@ def _lists(what, page_list, kv_lens, dev) -> Tuple[int, int]:
 
 def _places(what, name, t, dtype, batch, capacity, dev):
     """Checks a tensor of a value a place, [batch][places], of which a call takes the first `capacity`."""
-    if not (t.dtype is dtype and len(t.shape) == 2 and t.shape[0] == batch and t.shape[1] >= capacity and
-            (t.stride(1) == 1 or t.shape[1] < 2) and t.get_device() == dev):
+    shape = t.shape
+    if not (t.dtype is dtype and len(shape) == 2 and shape[0] == batch and shape[1] >= capacity and
+            (t.stride(1) == 1 or shape[1] < 2) and t.get_device() == dev):
         _bad(what, f"{name} must be {dtype} [{batch}][{capacity} or more], places contiguous, on device {dev}, not {_is(t)}")
 
 
@@ -428,22 +429,28 @@ def evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_list: torch.Tensor,
         _bad(what, f"v_cache must be like k_cache, {dtype} {tuple(cache)} on device {dev}, not {_is(v_cache)}")
     batch, entries = _lists(what, page_list, kv_lens, dev)
     capacity = entries * cache[1]
-    for name, t in (("keep", keep), ("since", since), ("lens_out", lens_out)):
-        if t is not None and not (t.dtype is _I32 and t.shape == (batch,) and t.is_contiguous() and t.get_device() == dev):
-            _bad(what, f"{name} must be a contiguous int32 [{batch}] on device {dev}, not {_is(t)}")
+    one = kv_lens.shape
+    if not (keep.dtype is _I32 and keep.shape == one and keep.is_contiguous() and keep.get_device() == dev):
+        _bad(what, f"keep must be a contiguous int32 [{batch}] on device {dev}, not {_is(keep)}")
+    if since is not None and not (since.dtype is _I32 and since.shape == one and since.is_contiguous() and
+                                  since.get_device() == dev):
+        _bad(what, f"since must be a contiguous int32 [{batch}] on device {dev}, not {_is(since)}")
+    if lens_out is None:
+        lens_out = torch.empty_like(kv_lens)
+    elif not (lens_out.dtype is _I32 and lens_out.shape == one and lens_out.is_contiguous() and
+              lens_out.get_device() == dev):
+        _bad(what, f"lens_out must be a contiguous int32 [{batch}] on device {dev}, not {_is(lens_out)}")
     _places(what, "mass", mass, _F32, batch, capacity, dev)
     if positions is not None:
         _places(what, "positions", positions, _I32, batch, capacity, dev)
-    if lens_out is None:
-        lens_out = torch.empty_like(kv_lens)
     if mass_out is None:
         mass_out = torch.empty_like(mass if mass.shape[1] == capacity else mass[:, :capacity])
-    else:
+    elif mass_out is not mass:
         _places(what, "mass_out", mass_out, _F32, batch, capacity, dev)
     if positions_out is None:
         positions_out = (torch.empty_like(mass_out, dtype=_I32) if positions is None or positions.shape[1] != capacity else
                          torch.empty_like(positions))
-    else:
+    elif positions_out is not positions:
         _places(what, "positions_out", positions_out, _I32, batch, capacity, dev)
     kc, vc = k_cache.stride(), v_cache.stride()
     if not kc[3] == vc[3] == 1:
