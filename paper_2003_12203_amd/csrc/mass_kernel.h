@@ -446,6 +446,18 @@ struct MassRuns {
             const MassSeq sq(a, b);
             incl = sq.nq > 0 ? (sq.kv - sq.first(a) + keys - 1) / keys : 0;
         }
+        if (a.capacity <= 1 << 29) {   // 64 sequences' blocks, of 16 keys at least, are fewer than 2^32
+            uint32_t x = (uint32_t)incl;
+#define FT_SCAN(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, false)
+            FT_SCAN(0x111, 0xf);   // row_shr 1, 2, 4, 8
+            FT_SCAN(0x112, 0xf);
+            FT_SCAN(0x114, 0xf);
+            FT_SCAN(0x118, 0xf);
+            FT_SCAN(0x142, 0xa);   // the last of rows 0 and 2 to rows 1 and 3, of row 1 to rows 2 and 3
+            FT_SCAN(0x143, 0xc);
+#undef FT_SCAN
+            return x;
+        }
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) {
             const long long v = __shfl_up(incl, x);
@@ -514,6 +526,9 @@ __global__ __launch_bounds__(256, (MassFew<T, DP>::WAVES)) void mass_few_kernel(
         tokens_that_see(a, sq, k0, k1, i0, i1);
         const int r0 = uniform(i0 * a.group / 16), r1 = uniform((i1 * a.group + 15) / 16);   // tiles of 16 rows
         const int32_t *list = a.page_list + (long long)b * a.list_stride;
+        static_assert(BLOCK <= 256, "a thread has a key");
+        float *to = p.mass + b * p.mass_stride + k0;
+        const float before = to[min((int)threadIdx.x, k1 - k0 - 1)];
         const char *krow[TILES][S2];
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
@@ -615,9 +630,8 @@ __global__ __launch_bounds__(256, (MassFew<T, DP>::WAVES)) void mass_few_kernel(
                     if (n16 == 0) sums[w][t * KEYS + 16 * s + 4 * h + i] = v;
                 }
         __syncthreads();
-        float *to = p.mass + b * p.mass_stride;
-        for (int j = threadIdx.x; j < k1 - k0; j += 256)
-            to[k0 + j] += ((sums[0][j] + sums[1][j]) + sums[2][j]) + sums[3][j];
+        const int j = threadIdx.x;
+        if (j < k1 - k0) to[j] = before + (((sums[0][j] + sums[1][j]) + sums[2][j]) + sums[3][j]);
     }
 }
 
