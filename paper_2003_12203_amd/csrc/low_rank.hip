@@ -579,8 +579,9 @@ __device__ __forceinline__ void copy_rows(const LowRankArgs &a, const TileTokens
     }
 }
 
-// Outputs m0 on up to m1, in `steps` of 64, of a tile's tokens with an adapter, by a wave.  load_low: h, after the first loads.
-template <typename T, int MT, int RC, bool GROUPED, typename F>
+// Outputs m0 on up to m1, in `steps` of 64, of a tile's tokens with an adapter, by a wave.  load_low: h, after the first loads (EARLY)
+// or before them.
+template <typename T, int MT, int RC, bool GROUPED, bool EARLY, typename F>
 __device__ __forceinline__ void expand_tile(const LowRankArgs &a, int adapter, const TileTokens &tokens, int m0, int m1, int steps, float *room,
                                             F load_low) {
     using C = Chunk<T>;
@@ -602,10 +603,11 @@ __device__ __forceinline__ void expand_tile(const LowRankArgs &a, int adapter, c
     };
     Low<T, MT, RC> low;
     Rows y0, y1;
+    if constexpr (!EARLY) load_low(low);
     rows.load(y0, m0);
 #pragma unroll
     for (int q = 0; q < 4; ++q) load_b(q, 0);
-    load_low(low);
+    if constexpr (EARLY) load_low(low);
     const int edge = rank / C::VALUES;   // the chunk that the rank ends in, and what of it counts
     const uint4 inside = within_rank<T>(make_uint4(~0u, ~0u, ~0u, ~0u), (4 * edge + h) * EU, rank);
     auto go = [&](auto all) __attribute__((always_inline)) {
@@ -655,7 +657,7 @@ __global__ __launch_bounds__(256, MT * RC * (int)sizeof(T) <= 8 ? 2 : 1) void ex
     if (m0 >= m1) return;
     auto tile_of = [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
         if (adapter < 0) return copy_rows<T>(a, tokens, TILE, m0, m1);
-        expand_tile<T, MT, RC, GROUPED>(a, adapter, tokens, m0, m1, (m1 - m0 + 63) / 64, room[w], [&](auto &low) __attribute__((always_inline)) {
+        expand_tile<T, MT, RC, GROUPED, true>(a, adapter, tokens, m0, m1, (m1 - m0 + 63) / 64, room[w], [&](auto &low) __attribute__((always_inline)) {
             low.load(a, a.splits, [&](int i) { return a.low + (long long)tokens.token(i) * a.rank; });
         });
     };
@@ -685,7 +687,8 @@ template <typename T, int NB> __global__ __launch_bounds__(64 * kShrinkWaves) vo
     const int steps = (m1 - from + 63) / 64, m0 = steps ? from : 0;   // (a wave without outputs takes part in h)
     each_adapter<16>(a, (int)x2, (int)(x1 - x2 * a.expand_ways), a.expand_ways, [&](int adapter, const TileTokens &tokens) __attribute__((always_inline)) {
         if (adapter < 0) return copy_rows<T>(a, tokens, 16, from, m1);
-        expand_tile<T, 1, RC, false>(a, adapter, tokens, m0, m1, steps, sums + w * TileRows<T, 1>::ROOM, [&](auto &low) __attribute__((always_inline)) {
+        // (the first outputs' loads beside the products with A, where registers hold both)
+        expand_tile<T, 1, RC, false, NB * (int)sizeof(T) <= 8>(a, adapter, tokens, m0, m1, steps, sums + w * TileRows<T, 1>::ROOM, [&](auto &low) __attribute__((always_inline)) {
             S::parts(a, adapter, tokens, 0, 0, sums);
             const int rank = used_rank(a, adapter);
             const float s = a.scales ? a.scales[adapter] : 1.0f;
@@ -745,17 +748,18 @@ template <typename T, int NB> hipError_t both_go(const LowRankPlan &pl, const Lo
 template <typename T> hipError_t pick(const LowRankPlan &pl, const LowRankArgs &a, hipStream_t st) {
     if (pl.both) {
         if constexpr (sizeof(T) == 2)
-            if (pl.blocks == 4) return both_go<T, 4>(pl, a, st);
+            if (pl.blocks == 8) return both_go<T, 8>(pl, a, st);
+        if (pl.blocks == 4) return both_go<T, 4>(pl, a, st);
         return pl.blocks == 1 ? both_go<T, 1>(pl, a, st) : both_go<T, 2>(pl, a, st);
     }
     if (pl.grouped) return pl.tile == 16 ? go<T, 1, true>(pl, a, st) : go<T, 2, true>(pl, a, st);
     return pl.tile == 16 ? go<T, 1, false>(pl, a, st) : go<T, 2, false>(pl, a, st);
 }
 
-// Calls of one launch: so many tokens, bytes that a workgroup reads for a tile's h, and so large a rank in bf16 (half in fp32),
+// Calls of one launch: so many tokens, bytes that a workgroup reads for a tile's h, and all of them do, and bytes of a row of B,
 // past which registers spill.
-constexpr int kBothTokens = 64, kBothRank = 64;
-constexpr long long kBothBytes = 1 << 18;
+constexpr int kBothTokens = 512, kBothRank = 256;
+constexpr long long kBothBytes = 1 << 18, kBothAll = 24 << 20;
 
 // Bins of group_kernel, two counts each, that LDS holds without more of it being asked for.
 constexpr int kMaxBins = 8000;
@@ -792,20 +796,25 @@ LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d) {
     // ranges of channels where there are too few workgroups still: four chunks of 64 bytes a wave at least
     const long long chunks = ((long long)d.ch * (d.dtype == FTCNN_F32 ? 4 : 2) + 63) / 64;
     p.splits = (int)std::max(1LL, std::min(chunks / (4 * kShrinkWaves), (p.grouped ? 1LL : 2LL) * kComputeUnits / ((long long)p.tiles * p.groups * p.ways)));
-    // One launch where every workgroup can have its tile's h for itself: 256 KB to read for it at most (16 tokens of 4096 channels,
-    // rank 16, read that: 10.3 us, in two launches 9.2, and 13 from the host).
-    const long long es = d.dtype == FTCNN_F32 ? 4 : 2;
-    p.both = !p.grouped && d.tokens <= kBothTokens && d.rank <= kBothRank * 2 / es && (d.rank + std::min(d.tokens, 16)) * (long long)d.ch * es <= kBothBytes;
-    if (p.both) {
+    // One launch where every workgroup can have its tile's h for itself: 256 KB to read for it at most, and 24 MB for all tiles,
+    // adapters and spans of outputs.  (From the host; with two launches each takes 12 to 13 us: 16 tokens of 4096 channels and
+    // rank 16, 256 KB, 10.6; 512 tokens of 128 channels and outputs, 8 adapters of rank 16, 8.2; of 1024 and 2048, rank 32,
+    // 100 MB, 15.9, and 13.5 with two.)
+    const long long es = d.dtype == FTCNN_F32 ? 4 : 2, low = (d.rank + std::min(d.tokens, 16)) * (long long)d.ch * es;
+    if (!p.grouped && d.tokens <= kBothTokens && d.rank * es <= kBothRank && low <= kBothBytes) {
         const long long waves = ((d.m + 63) / 64 + kShrinkWaves - 1) / kShrinkWaves;
-        p.blocks = rows > 2 ? 4 : rows;
-        p.groups = p.splits = p.together = 1;
-        p.expand_ways = share(kComputeUnits, p.tiles);
-        const long long spans = std::max(1LL, std::min(waves, 2LL * kComputeUnits / ((long long)p.tiles * p.expand_ways)));
-        const long long each = (waves + spans - 1) / spans;
-        p.columns = (int)(64 * each);
-        p.spans = (int)((waves + each - 1) / each);
-        return p;
+        const int ways = share(kComputeUnits, p.tiles);
+        const long long most_spans = std::max(1LL, std::min(waves, 2LL * kComputeUnits / ((long long)p.tiles * ways)));
+        const long long each = (waves + most_spans - 1) / most_spans, spans = (waves + each - 1) / each;
+        p.both = p.tiles * std::min<long long>(most, d.tokens) * spans * low <= kBothAll;
+        if (p.both) {
+            p.blocks = rows > 4 ? 8 : (rows > 2 ? 4 : rows);
+            p.groups = p.splits = p.together = 1;
+            p.expand_ways = ways;
+            p.columns = (int)(64 * each);
+            p.spans = (int)spans;
+            return p;
+        }
     }
     // The second launch: as many spans of 64 outputs as fill two workgroups to a compute unit, and no second round of them.
     const long long blocks = (d.m + 63) / 64;

@@ -45,7 +45,8 @@ SIZES = [  # tokens, ch, m, adapters, rank: each tile size, ranks of each compil
     (1, 64, 64, 1, 8), (1, 4096, 6144, 8, 16), (2, 8, 8, 3, 8), (15, 40, 72, 4, 16), (16, 4096, 264, 16, 32),
     (17, 1000, 1288, 5, 24), (64, 512, 512, 48, 40), (65, 264, 136, 2, 64), (130, 128, 1032, 7, 128), (256, 96, 64, 3, 72),
     (257, 264, 328, 9, 16), (300, 72, 2056, 4, 64), (320, 2048, 40, 1, 8), (511, 136, 200, 70, 24), (290, 512, 104, 3, 128),
-    (600, 88, 96, 2, 104)]
+    (600, 88, 96, 2, 104), (700, 72, 136, 3, 8), (700, 264, 72, 3, 24), (700, 72, 136, 40, 64), (700, 72, 136, 3, 128),
+    (17, 8192, 64, 5, 16), (40, 6000, 1032, 9, 72), (5, 4104, 520, 3, 128), (513, 64, 64, 2, 16), (512, 64, 64, 2, 16)]
 
 
 @pytest.mark.parametrize("tokens,ch,m,count,rank", SIZES)
@@ -65,6 +66,7 @@ def test_tokens_grouped(tokens, ch, m, count, rank, dtype):
 
 
 MANY = [(4100, 72, 80, 2, 8), (4100, 72, 80, 2, 24), (4100, 72, 80, 2, 64), (8200, 40, 40, 2, 128), (4100, 40, 40, 130, 72),
+        (4100, 16, 16, 130, 72), (4100, 16, 16, 130, 40), (4100, 40, 40, 130, 24), (4100, 40, 40, 130, 40), (4100, 40, 40, 130, 8),
         (4100, 64, 64, 8001, 8), (2049, 2048, 1032, 1, 48), (8200, 520, 264, 1, 16)]
 
 
@@ -92,7 +94,7 @@ def test_fp32_sizes_of_four(rank, ch, m):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("tokens", [40, 400, 9000])
+@pytest.mark.parametrize("tokens", [40, 400, 700, 9000])
 def test_ranks_and_what_lies_past_them(tokens, dtype):
     """Ranks of every kind, NaN past them, and adapters that no token has."""
     s = make(3, tokens, 200, 144, 9, 24, dtype)
@@ -108,7 +110,7 @@ def test_ranks_and_what_lies_past_them(tokens, dtype):
     check(clean, got, dtype, ranks)
 
 
-@pytest.mark.parametrize("tokens,ch,m,count", [(20, 96, 80, 3), (300, 96, 80, 3), (2100, 1000, 600, 16), (4100, 520, 264, 17)])
+@pytest.mark.parametrize("tokens,ch,m,count", [(20, 96, 80, 3), (300, 96, 80, 3), (700, 96, 80, 3), (2100, 1000, 600, 16), (4100, 520, 264, 17)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_values_that_are_not_finite_reach_only_their_token(tokens, ch, m, count, dtype):
     s = make(4, tokens, ch, m, count, 16, dtype)
@@ -133,7 +135,7 @@ def test_ids_out_of_range_are_no_adapter(dtype):
     assert torch.equal(adapters.low_rank_add(**s), s["y"])
 
 
-@pytest.mark.parametrize("tokens", [9, 270, 25000])
+@pytest.mark.parametrize("tokens", [9, 270, 700, 25000])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_layouts(tokens, dtype):
     """Slices of packed rows, weights inside larger ones, in place, an output with rows of its own."""
@@ -170,7 +172,7 @@ def test_rows_past_32_bits():
     assert torch.equal(adapters.low_rank_add(y, x, a, b, s["ids"], s["scales"], out=y), want)
 
 
-@pytest.mark.parametrize("tokens,count", [(1, 4), (50, 20), (700, 40), (6000, 40)])
+@pytest.mark.parametrize("tokens,count", [(1, 4), (50, 20), (700, 3), (700, 40), (6000, 40)])
 def test_same_bits_streams_and_graphs(tokens, count):
     s = make(8, tokens, 640, 512, count, 32, "bf16")
     want = adapters.low_rank_add(**s)
@@ -219,7 +221,7 @@ def test_binding_refuses():
         with pytest.raises(ft.FtcnnError, match="low_rank_add"):
             adapters.low_rank_add(**s, **kw)
     with pytest.raises(ft.FtcnnError, match="low_rank_add: the workspace"):
-        adapters.low_rank_add(**make(10, 200, 64, 64, 2, 16, "bf16"), workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        adapters.low_rank_add(**make(10, 600, 64, 64, 2, 16, "bf16"), workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ft.FtcnnError, match="16 bytes"):
         adapters.low_rank_add(**{**s, "x": torch.zeros(6, 72, dtype=torch.bfloat16, device="cuda")[:, 4:68]})
     with pytest.raises(ft.FtcnnError, match="no backward"):

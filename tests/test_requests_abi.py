@@ -76,7 +76,7 @@ def test_low_rank_add_refuses(kw, code):
 
 
 def test_low_rank_add_takes_fp32_sizes_of_four():
-    assert _lib.load().ftcnn_low_rank_workspace_bytes(bytes(low_rank(dict(dtype=0, ch=60, m=4, rank=12, tokens=500)))) > 0
+    assert _lib.load().ftcnn_low_rank_workspace_bytes(bytes(low_rank(dict(dtype=0, ch=60, m=4, rank=12, tokens=5000)))) > 0
 
 
 @pytest.mark.parametrize("kw", [dict(y=None), dict(x=None), dict(a=None), dict(b=None), dict(ids=None), dict(out=None)])
@@ -99,11 +99,10 @@ def test_low_rank_add_workspace():
     for tokens in (1, 16, 17, 256, 257, 8192, 1 << 20):
         for rank in (8, 64, 128):
             need = L.ftcnn_low_rank_workspace_bytes(bytes(low_rank(dict(tokens=tokens, rank=rank))))
-            small = tokens <= 17 and rank <= 64   # one launch, which needs none
-            assert need == 0 if small else need % 256 == 0 and need >= tokens * rank * 4
+            assert need == 0 if tokens <= 257 else need % 256 == 0 and need >= tokens * rank * 4
     assert L.ftcnn_low_rank_workspace_bytes(None) == 0 and L.ftcnn_low_rank_workspace_bytes(bytes(low_rank(dict(tokens=0)))) == 0
-    assert call_low_rank(low_rank(dict(tokens=500)), ws=None) == E_WORKSPACE
-    assert call_low_rank(low_rank(dict(tokens=500)), ws=C.c_void_p((1 << 20) + 16)) == E_WORKSPACE
+    assert call_low_rank(low_rank(dict(tokens=5000)), ws=None) == E_WORKSPACE
+    assert call_low_rank(low_rank(dict(tokens=5000)), ws=C.c_void_p((1 << 20) + 16)) == E_WORKSPACE
 
 
 @pytest.mark.parametrize("kw,code", [
