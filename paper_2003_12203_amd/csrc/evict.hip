@@ -12,7 +12,7 @@
 // part_kernel: five launches for longer ones, a workgroup for every 8192 places: three count bits, each with the limit from
 // the counts of the one before in all parts, one counts what moves, one writes.  131072 rows halved: 36 us (49 in parts of
 // 16384, 36 in parts of 4096; of 64 sequences of 32768 46, 52 in parts of 4096).
-// move_kernel: the moves' rows of all heads, keys and values, 16 bytes a lane, four moves on their way.  The same 131072 rows:
+// move_kernel: the moves' rows of all heads, keys and values, 16 bytes a lane, two moves on their way.  The same 131072 rows:
 // 62 us, 4.3 TB/s read and written.
 #include <algorithm>
 
@@ -437,7 +437,8 @@ template <int STEP> __global__ __launch_bounds__(kSelect) void part_kernel(Evict
 }
 
 __global__ __launch_bounds__(kThreads) void move_kernel(EvictArgs a) {
-    constexpr int AHEAD = 4;   // moves on their way
+    constexpr int AHEAD = 2;   // moves on their way (64 sequences of 4097, a move each: 4.2 us; four on their way 5.6, one 4.1, but 131072
+                               // rows halved 66 where two take 61)
     const int b = (int)(blockIdx.x / (unsigned)a.shares), share = (int)(blockIdx.x % (unsigned)a.shares);
     const int moves = a.counts[b];
     if (a.parts) {   // the weights and positions that move, and the length, which nobody else reads here

@@ -400,7 +400,7 @@ int ftcnn_evict(const ftcnn_evict_desc *d, void *k_cache, void *v_cache, const i
     e.part = reinterpret_cast<EvictPart *>(ws + room.part);
     e.div_page = fast_div((uint32_t)d->page);
     // workgroups of a sequence: four rows of its moves each at a time, 2048 in all (64 sequences of 32768 rows of 256 bytes
-    // halved 123 us, 132 with 1024; where next to nothing moves those that find nothing cost 1.4 us more)
+    // halved 123 us, 132 with 1024; those that find nothing to move cost a microsecond)
     const long long longest = evict_longest(*d);
     e.held = (int)std::min<long long>(room.parts ? kEvictPart : kEvictHeld, std::max(1024LL, (longest + 1023) / 1024 * 1024));
     const long long together = std::max(1LL, (long long)kThreads / (2LL * d->kv_heads * e.units));
