@@ -255,6 +255,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) * KS <= 512 ? 2 : 1) void mass_
         unit[i] = slot ^ L::key_unit(r);
         place[i] = (unsigned)(r >> shift) * (unsigned)(a.qs[0] * sizeof(T)) + (unsigned)(r & few) * (unsigned)(a.qs[1] * sizeof(T)) + unit[i] * 16;
     }
+    // log-sums 32 rows on (shift 6: a token's heads)
+    const unsigned log_step = shift < 6 ? (unsigned)(32 >> shift) * (unsigned)heads : 32;
     const T *q0 = static_cast<const T *>(a.q) + (long long)sq.q0 * a.qs[0];
     const float *lse0 = p.lse + (long long)sq.q0 * heads;
 
@@ -310,12 +312,11 @@ __global__ __launch_bounds__(256, DP * sizeof(T) * KS <= 512 ? 2 : 1) void mass_
                 if (issued < u1) {
                     const unsigned to = lds_at + ((issued - u0) & 1) * L::SIDE + w * OWN * RB;
                     if (p.near && coming.tile < full) {
+                        int r = l32;
+                        asm volatile("" : "+v"(r));   // here: the offset would not find a register across the loop
+                        const unsigned log_at = (unsigned)(r >> shift) * (unsigned)heads + (r & few);
 #pragma unroll
-                        for (int i = 0; i < QS; ++i) {
-                            int r = 32 * i + l32;
-                            asm volatile("" : "+v"(r));   // here: its offset would not find a register across the loop
-                            next_log[i] = lse_at[(unsigned)(r >> shift) * (unsigned)heads + (r & few)];
-                        }
+                        for (int i = 0; i < QS; ++i) next_log[i] = lse_at[log_at + i * log_step];
 #pragma unroll
                         for (int i = 0; i < L::LOADS; ++i) {
                             if (DP != a.dim && (int)unit[i] * EU >= a.dim) continue;
