@@ -8,12 +8,12 @@
 // with next to no work: loops over places in LDS are short code (held in registers they were straight code, 16 us for 64
 // sequences of 4097 against 12 now), without branches, and sums over lanes and waves go through DPP.
 //
-// select_kernel: a workgroup a sequence, which keeps up to 16384 places in LDS.  64 sequences of 4097 rows, one out: 11.8 us.
+// select_kernel: a workgroup a sequence, which keeps up to 16384 places in LDS.  64 sequences of 4097 rows, one out: 11.5 us.
 // part_kernel: five launches for longer ones, a workgroup for every 8192 places: three count bits, each with the limit from
-// the counts of the one before in all parts, one counts what moves, one writes.  131072 rows halved: 36 us (49 in parts of
+// the counts of the one before in all parts, one counts what moves, one writes.  131072 rows halved: 34 us (49 in parts of
 // 16384, 36 in parts of 4096; of 64 sequences of 32768 46, 52 in parts of 4096).
 // move_kernel: the moves' rows of all heads, keys and values, 16 bytes a lane, two moves on their way.  The same 131072 rows:
-// 62 us, 4.3 TB/s read and written.
+// 61 us, 4.4 TB/s read and written.
 #include <algorithm>
 
 #include "evict.h"
