@@ -411,8 +411,9 @@ def evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_list: torch.Tensor,
     """ftcnn_evict: of each sequence's kv_lens rows keep (int32 [batch]) stay, those at positions below `first` or
     from since (int32 [batch]) on and then those of the largest mass (float32 [batch][places]).  Rows that stay move into
     places that become free, so the caches change, and a row's position is no longer its place: positions (int32
-    [batch][places]; None: still the places) say which it is.  Returns the new (lens, mass, positions), allocated
-    unless given (in place: lens_out=kv_lens, mass_out=mass, positions_out=positions).  No page may be listed twice.
+    [batch][places]; None: still the places) say which it is.  Returns the new (lens, mass, positions), allocated, with a place
+    for each row that a page list can name, unless given (in place: lens_out=kv_lens, mass_out=mass, positions_out=positions;
+    places past those are left as they were).  No page may be listed twice.
     workspace: uint8, 256-byte aligned; allocated when not given."""
     what = "evict"
     dtype, cache, dev = k_cache.dtype, k_cache.shape, k_cache.get_device()
@@ -448,8 +449,10 @@ def evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_list: torch.Tensor,
     elif mass_out is not mass:
         _places(what, "mass_out", mass_out, _F32, batch, capacity, dev)
     if positions_out is None:
-        positions_out = (torch.empty_like(mass_out, dtype=_I32) if positions is None or positions.shape[1] != capacity else
-                         torch.empty_like(positions))
+        # (of other widths than the lists': what the call does not write would be anything)
+        positions_out = (torch.empty_like(positions) if positions is not None and positions.shape[1] == capacity else
+                         torch.empty_like(mass_out, dtype=_I32) if mass_out.shape[1] == capacity else
+                         mass_out.new_empty((batch, capacity), dtype=_I32))
     elif positions_out is not positions:
         _places(what, "positions_out", positions_out, _I32, batch, capacity, dev)
     kc, vc = k_cache.stride(), v_cache.stride()

@@ -284,3 +284,21 @@ def test_binding_refuses():
             paged.evict(**args, **kw)
     with pytest.raises(ft.FtcnnError, match="no backward"):
         paged.evict(**{**args, "mass": s["mass"].clone().requires_grad_()})
+
+
+@pytest.mark.parametrize("positions", [False, True])
+@pytest.mark.parametrize("given", ["none", "mass", "other"])
+def test_allocated_positions_have_the_lists_places(given, positions):
+    """Whatever the width of the weights that are given and of the positions that are read: a place for every row that the lists can
+    name, and each of them written."""
+    s = make(15, [200, 0, 70], [90, 5, 69], positions=True)
+    places = s["mass"].shape[1]
+    wide = {k: torch.nn.functional.pad(s[k], (0, 33), value=5) for k in ("mass", "positions")}
+    t = dict(s, k=s["k"].clone(), v=s["v"].clone(), mass=wide["mass"], positions=wide["positions"] if positions else None)
+    want = check(s if positions else dict(s, positions=None), 4)
+    mass_out = {"none": None, "mass": t["mass"], "other": torch.full_like(wide["mass"], 7.0)}[given]
+    lens, mass, pos = run(t, first=4, mass_out=mass_out)
+    assert pos.shape == (3, places) and pos.dtype == torch.int32
+    assert torch.equal(pos, want[2]) and torch.equal(mass[:, :places], want[1]) and torch.equal(lens, want[0])
+    assert mass.shape == ((3, places) if given == "none" else wide["mass"].shape)
+    assert given == "none" or (mass[:, places:] == (5 if given == "mass" else 7)).all()   # what is not the lists' is left
