@@ -120,6 +120,14 @@ def _places(what, name, t, dtype, batch, capacity, dev):
         _bad(what, f"{name} must be {dtype} [{batch}][{capacity} or more], places contiguous, on device {dev}, not {_is(t)}")
 
 
+def _like(t, batch, capacity, dtype):
+    """A new tensor of a value a place that the call's lists can name, in the rows that the kernels write: t may have others, or wider
+    or overlapping ones, which empty_like would follow."""
+    if t.shape[1] == capacity and t.is_contiguous():   # (the quicker call)
+        return torch.empty_like(t, dtype=dtype)
+    return t.new_empty((batch, capacity), dtype=dtype)
+
+
 def rope_table(max_pos: int, rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
                original: int = 0, low: float = 1.0, high: float = 32.0, amplitude: float = 1.0, device="cuda",
                stream=None) -> torch.Tensor:
@@ -445,14 +453,11 @@ def evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_list: torch.Tensor,
     if positions is not None:
         _places(what, "positions", positions, _I32, batch, capacity, dev)
     if mass_out is None:
-        mass_out = torch.empty_like(mass if mass.shape[1] == capacity else mass[:, :capacity])
+        mass_out = _like(mass, batch, capacity, _F32)
     elif mass_out is not mass:
         _places(what, "mass_out", mass_out, _F32, batch, capacity, dev)
     if positions_out is None:
-        # (of other widths than the lists': what the call does not write would be anything)
-        positions_out = (torch.empty_like(positions) if positions is not None and positions.shape[1] == capacity else
-                         torch.empty_like(mass_out, dtype=_I32) if mass_out.shape[1] == capacity else
-                         mass_out.new_empty((batch, capacity), dtype=_I32))
+        positions_out = _like(mass_out if positions is None else positions, batch, capacity, _I32)
     elif positions_out is not positions:
         _places(what, "positions_out", positions_out, _I32, batch, capacity, dev)
     kc, vc = k_cache.stride(), v_cache.stride()

@@ -302,3 +302,19 @@ def test_allocated_positions_have_the_lists_places(given, positions):
     assert torch.equal(pos, want[2]) and torch.equal(mass[:, :places], want[1]) and torch.equal(lens, want[0])
     assert mass.shape == ((3, places) if given == "none" else wide["mass"].shape)
     assert given == "none" or (mass[:, places:] == (5 if given == "mass" else 7)).all()   # what is not the lists' is left
+
+
+def test_weights_and_positions_of_overlapping_rows():
+    """Windows of one array, a place apart or the same for all, are read like any others, and what is allocated has rows of its own."""
+    s = make(16, [60, 64, 33], [20, 63, 30], extra=0)
+    places = s["mass"].shape[1]
+    base = torch.rand(places + 2, generator=torch.Generator().manual_seed(1)).cuda()
+    for mass, pos in ((base.unfold(0, places, 1), torch.arange(5, places + 7, dtype=torch.int32, device="cuda").unfold(0, places, 1)),
+                      (base[:places].expand(3, -1), torch.arange(places, dtype=torch.int32, device="cuda").expand(3, -1))):
+        assert mass.stride(0) < 2 and pos.stride(0) < 2
+        for positions in (pos, None):
+            t = dict(s, k=s["k"].clone(), v=s["v"].clone(), mass=mass, positions=positions)
+            want = check(dict(t, k=t["k"].clone(), v=t["v"].clone(), mass=mass.contiguous(),
+                              positions=None if positions is None else positions.contiguous()), 6)
+            got = check(t, 6)
+            assert all(torch.equal(a, b) and a.is_contiguous() for a, b in zip(got, want))
