@@ -433,6 +433,7 @@ __device__ __forceinline__ void narrow(uint16_t &d, float v) { d = f32_to_bf16_r
 //
 // bf16: h is the sum of two bf16 values (an error of 2^-17 of it; rounded to one, its products would be off by as
 // much as the outputs' own rounding).
+constexpr float kLargest = 0x1.fep127f;   // of bf16
 __device__ __forceinline__ int output_row(int n16, int q) { return 16 * (n16 >> 2) + 4 * q + (n16 & 3); }
 
 // h of a tile's tokens, as operands: unit c * 4 + h of token 16 i + n16.  (Of tokens that are none, of others: their products go
@@ -490,9 +491,14 @@ template <typename T, int MT, int RC> struct Low {
                 Unit<T> hi, lo;
 #pragma unroll
                 for (int e = 0; e < EU; ++e) {
-                    narrow(hi.e[e], v[e]);
-                    const float top = widen(hi.e[e]);
-                    narrow(lo.e[e], fabsf(top) < INFINITY ? v[e] - top : 0.0f);   // (of an infinity or NaN there is no rest)
+                    if constexpr (PLANES == 1) {
+                        hi.e[e] = v[e];
+                    } else {
+                        // what would round to an infinity: the largest bf16 value and the rest; of an infinity or NaN there is no rest
+                        const bool finite = fabsf(v[e]) < INFINITY;
+                        narrow(hi.e[e], finite ? fminf(fmaxf(v[e], -kLargest), kLargest) : v[e]);
+                        narrow(lo.e[e], finite ? v[e] - widen(hi.e[e]) : 0.0f);
+                    }
                 }
                 low[i][c][0] = hi.q;
                 if constexpr (PLANES == 2) low[i][c][PLANES - 1] = lo.q;

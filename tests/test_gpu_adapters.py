@@ -230,3 +230,34 @@ def test_binding_refuses():
         adapters.low_rank_add(**{**s, "x": s["x"].clone().requires_grad_()})
     none = adapters.low_rank_add(s["y"][:0], s["x"][:0], s["a"], s["b"], s["ids"][:0])
     assert none.shape == (0, 64)
+
+
+@pytest.mark.parametrize("tokens,ch,m,count", [(1, 64, 64, 3), (40, 200, 144, 3), (700, 64, 64, 3), (2100, 1000, 600, 40), (4100, 1000, 600, 17)])
+@pytest.mark.parametrize("rank", [16, 72])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_products_beyond_the_largest_bf16_value(tokens, ch, m, count, rank, dtype):
+    """A x between the largest bf16 value and the largest fp32 one: +-(2 - 2^-7 + 3 * 2^-9) 2^127, with B so small that outputs are
+    ordinary numbers.  As two bf16 values it is within 2^-17 of itself, like any other."""
+    s = make(tokens + rank, tokens, ch, m, count, rank, dtype, none=0.0)
+    sign = torch.where(torch.arange(rank) % 3 == 1, -1.0, 1.0).to("cuda", DT[dtype])
+    s["x"].zero_(), s["a"].zero_()
+    s["x"][:, 0], s["x"][:, 1] = 2.0 ** 63, 2.0 ** 60
+    s["a"][:, :, 0], s["a"][:, :, 1] = sign * ((2 - 2.0 ** -7) * 2.0 ** 64), sign * (1.5 * 2.0 ** 59)
+    s["b"] *= 2.0 ** -120
+    s["scales"] = None
+    got = adapters.low_rank_add(**s)
+    assert got.isfinite().all()
+    check(s, got, dtype)
+
+
+@pytest.mark.parametrize("tokens,ch,m,count", [(3, 64, 64, 3), (700, 64, 64, 3), (2100, 1000, 600, 40), (4100, 1000, 600, 17)])
+def test_products_whose_rest_is_subnormal_in_bf16(tokens, ch, m, count):
+    """s A x = 2^-118 (1 + 5 * 2^-11), B = 2^110 and y = -2^-8: the rest beside 2^-118 is less than the least normal bf16 value, and
+    all that the output is."""
+    s = make(tokens, tokens, ch, m, count, 8, "bf16", none=0.0)
+    for k in ("x", "a", "b"):
+        s[k].zero_()
+    s["x"][:, 0], s["x"][:, 1] = 2.0 ** -9, 2.0 ** -14
+    s["a"][:, 3, 0], s["a"][:, 3, 1] = 2.0 ** -9, 1.25 * 2.0 ** -13
+    s["b"][:, :, 3], s["scales"][:], s["y"][:] = 2.0 ** 110, 2.0 ** -100, -2.0 ** -8
+    check(s, adapters.low_rank_add(**s), "bf16")
