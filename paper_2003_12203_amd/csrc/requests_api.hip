@@ -81,8 +81,10 @@ int check_low_rank(const ftcnn_low_rank_desc *d) {
         return set_error(FTCNN_E_SHAPE, "%s: more than 2^30 tokens, channels or outputs", what);
     if (d->tokens) {
         const LowRankPlan p = low_rank_plan(*d);
-        const long long one = (long long)p.tiles * p.ways * p.splits * p.groups, two = (long long)p.tiles * p.expand_ways * p.spans;
-        if (std::max(2 * one, two) > kMaxThreads / kThreads)
+        // (of 512 threads: the first launch, unless tokens are grouped, and the one for both products)
+        const long long one = p.both ? 0 : (long long)p.tiles * p.ways * p.splits * p.groups;
+        const long long two = (long long)((p.tiles + p.together - 1) / p.together) * p.expand_ways * p.spans;
+        if (std::max((p.grouped ? 1 : 2) * one, (p.both ? 2 : 1) * two) > kMaxThreads / kThreads)
             return set_error(FTCNN_E_SHAPE, "%s: %lld and %lld workgroups", what, one, two);
     }
     return FTCNN_OK;

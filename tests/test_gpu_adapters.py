@@ -261,3 +261,25 @@ def test_products_whose_rest_is_subnormal_in_bf16(tokens, ch, m, count):
     s["a"][:, 3, 0], s["a"][:, 3, 1] = 2.0 ** -9, 1.25 * 2.0 ** -13
     s["b"][:, :, 3], s["scales"][:], s["y"][:] = 2.0 ** 110, 2.0 ** -100, -2.0 ** -8
     check(s, adapters.low_rank_add(**s), "bf16")
+
+
+def test_as_many_grouped_tokens_as_are_launched():
+    """2^23 tokens of 7000 adapters: 8650752 tiles, more than half of what 2^32 threads of the first launch are."""
+    tokens, count, d = 1 << 23, 7000, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    y, x = (torch.randn(tokens, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    a, b = (torch.randn(count, d, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    ids = torch.randint(-1, count, (tokens,), generator=g, device="cuda").int()
+    scales = 0.25 + torch.rand(count, generator=g, device="cuda")
+    got = adapters.low_rank_add(y, x, a, b, ids, scales)
+    u32 = 2.0 ** -24
+    for t in range(0, tokens, 1 << 20):   # the definition and its bound (oracle.serving.low_rank_add), of many tokens together
+        part = slice(t, t + (1 << 20))
+        i = ids[part].clamp(min=0).long()
+        A, B, X, s = a[i].double(), b[i].double(), x[part].double()[:, None], (scales[i] * (ids[part] >= 0)).double()[:, None]
+        low, size = s * (A * X).sum(-1), s * (A * X).abs().sum(-1)
+        off = (d + 8) * u32 * size + 2.0 ** -16 * low.abs()
+        want, err = y[part].double() + (B * low[:, None]).sum(-1), (B.abs() * off[:, None]).sum(-1)
+        err = err + (d + 4) * u32 * ((B * low[:, None]).abs().sum(-1) + err)
+        assert ((got[part].double() - want).abs() <= err + (u32 + 2.0 ** -8) * (want.abs() + err)).all(), t
+    assert torch.equal(got[ids < 0], y[ids < 0])

@@ -202,3 +202,12 @@ def test_binding_refuses_host_tensors():
         paged.attention_mass(y, c[0, :2], c, i32.view(2, 1), i32, y)
     with pytest.raises(ft.FtcnnError, match="on a device"):
         paged.evict(c, c, i32.view(2, 1), i32, i32, y)
+
+
+def test_low_rank_add_takes_as_many_grouped_tokens_as_are_launched():
+    """A tile of the grouped launches is a workgroup of 256 threads in the first and a quarter of one in the second: 4096 parts of
+    2112 tiles are within 2^32 threads of each, 8192 of them are not."""
+    sizes = dict(ch=8, m=8, adapters=7000, rank=8, x_stride=8, y_stride=8, out_stride=8)
+    assert _lib.load().ftcnn_low_rank_workspace_bytes(bytes(low_rank(dict(sizes, tokens=1 << 23)))) > (1 << 23) * 8 * 4
+    assert call_low_rank(low_rank(dict(sizes, tokens=1 << 23)), ws=None) == E_WORKSPACE
+    assert call_low_rank(low_rank(dict(sizes, tokens=1 << 24))) == E_SHAPE
