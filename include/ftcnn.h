@@ -604,7 +604,8 @@ typedef struct {
  * positions, and lens_out may be kv_lens.  Cache rows from place k on keep what they held.
  * A page that rows of two sequences lie in, or that a list has twice, holds undefined values after it.  keep and kv_lens are
  * taken as at least 0, kv_lens as at most list_len * page, page numbers as in ftcnn_paged_attention.  Rows of the
- * cache start on 16 bytes; its strides are 0 to 2^29.  Two launches, or six where sequences are long. */
+ * cache start on 16 bytes, at most 2^29 units of 16 bytes of all key heads; its strides are 0 to 2^29.  Two launches, or
+ * six where sequences are long. */
 int ftcnn_evict(const ftcnn_evict_desc *desc, void *k_cache, void *v_cache, const int32_t *page_list, const int32_t *kv_lens,
                 const int32_t *keep, const float *mass, const int32_t *positions, const int32_t *since, int32_t *lens_out,
                 float *mass_out, int32_t *positions_out, void *workspace, hipStream_t stream);

@@ -119,6 +119,8 @@ int check_evict(const ftcnn_evict_desc *d) {
     rc = check_cache(what, d->batch, d->kv_heads, d->dim, d->pages, d->page, d->list_len);
     if (rc != FTCNN_OK) return rc;
     if ((long long)d->batch * 1024 > kMaxThreads) return set_error(FTCNN_E_SHAPE, "%s: %d sequences", what, d->batch);
+    if ((long long)d->kv_heads * (d->dim / vec_of(d->dtype)) > kMaxRows / 2)   // move_kernel counts those of keys and values
+        return set_error(FTCNN_E_SHAPE, "%s: %d key heads of %d", what, d->kv_heads, d->dim);
     return FTCNN_OK;
 }
 

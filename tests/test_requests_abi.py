@@ -211,3 +211,10 @@ def test_low_rank_add_takes_as_many_grouped_tokens_as_are_launched():
     assert _lib.load().ftcnn_low_rank_workspace_bytes(bytes(low_rank(dict(sizes, tokens=1 << 23)))) > (1 << 23) * 8 * 4
     assert call_low_rank(low_rank(dict(sizes, tokens=1 << 23)), ws=None) == E_WORKSPACE
     assert call_low_rank(low_rank(dict(sizes, tokens=1 << 24))) == E_SHAPE
+
+
+@pytest.mark.parametrize("kw", [dict(kv_heads=(1 << 29) + 1, dim=8), dict(kv_heads=1 << 30, dim=8), dict(kv_heads=1 << 24, dim=256, dtype=0)])
+def test_evict_refuses_rows_of_more_units_than_it_counts(kw):
+    """A row of all key heads, keys and values, is counted in 16-byte units in 31 bits."""
+    assert call_evict(evict(dict(kw, batch=1))) == E_SHAPE
+    assert "evict" in ft.last_error()
