@@ -318,3 +318,31 @@ def test_weights_and_positions_of_overlapping_rows():
                               positions=None if positions is None else positions.contiguous()), 6)
             got = check(t, 6)
             assert all(torch.equal(a, b) and a.is_contiguous() for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("moves", [6143, 6144, 6145, 8192])
+@pytest.mark.parametrize("kind", ["rising", "recent"])
+@pytest.mark.parametrize("positions", [False, True])
+def test_every_row_that_stays_moves(moves, kind, positions):
+    """16384 places, as many as a workgroup keeps in LDS, of which the last stay, for their weights or their positions: as many
+    moves as lists in LDS hold, one less and more, and the most that there are; in place as well."""
+    n = 16384
+
+    def fresh():
+        s = make(moves, [n, 30], [moves, 29], kv=1, dim=8, page=64, extra=0)
+        if kind == "rising":
+            s["mass"] = torch.arange(n, dtype=torch.float32, device="cuda").expand(2, n).contiguous()
+        if positions:
+            s["positions"] = torch.arange(n, dtype=torch.int32, device="cuda").expand(2, n).contiguous()
+        return s
+
+    s, t = fresh(), fresh()
+    since = torch.tensor([n - moves, 10], dtype=torch.int32, device="cuda") if kind == "recent" else None
+    want = check(s, 0, since, max_kv=n)
+    assert want[2][0, :moves].tolist() == list(range(n - moves, n))
+    held = dict(lens_out=t["lens"], mass_out=t["mass"])
+    if positions:
+        held["positions_out"] = t["positions"]
+    got = run(t, since=since, max_kv=n, **held)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    assert torch.equal(s["k"], t["k"]) and torch.equal(s["v"], t["v"])
