@@ -18,7 +18,7 @@ struct LowRankArgs {
     int tokens, ch, m, adapters, rank;
     int groups, splits;           // groups of rows of A, and ranges of channels, of workgroups of their own
     int ways, expand_ways;        // workgroups that share a tile's adapters, in either launch
-    int columns, tiles, together; // outputs of a wave of the second launch; tiles, and those of a workgroup of it
+    int columns;                  // outputs of a wave of the second launch
     int slots;                    // grouped: records of a part
     FastDiv div_slots;
     FastDiv div_groups, div_splits, div_ways, div_expand_ways, div_spans;
@@ -29,7 +29,8 @@ struct LowRankPlan {
     int parts, slots;             // ... in so many parts, of so many tiles at most
     int tile;                     // tokens of a tile
     int blocks;                   // rows of A of a workgroup, in 16
-    int tiles, groups, splits, ways, expand_ways, columns, together, spans;   // spans of outputs of the second's workgroups
+    int tiles, groups, splits, ways, expand_ways, columns;
+    int together, spans;          // tiles of a workgroup of the second launch; its workgroups' spans of outputs
     size_t records, order, count, bytes;   // workspace: after the products
 };
 LowRankPlan low_rank_plan(const ftcnn_low_rank_desc &d);

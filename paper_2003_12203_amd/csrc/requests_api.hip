@@ -169,7 +169,8 @@ MassPlan mass_plan(const ftcnn_mass_desc &d) {
         // Parts of at most 2^28 bytes.  A key head is a workgroup's, and its rows are shared by so many that there are two
         // workgroups to a compute unit, of two tiles of 64 rows at least, or eight, so that long ones even out, of eight
         // tiles (two prompts of 8192 tokens 560 us, four 602; 512 tokens over 8704 keys, which have 32 tiles, 61 with four
-        // workgroups to a compute unit, 73 with eight).
+        // workgroups to a compute unit, 73 with eight).  Parts are rounded up: workgroups that are a few more than the device holds
+        // at a time take another round (129 tokens over 22677 keys, one key head: 540, of which 512 at a time).
         const long long room = (1LL << 26) / (d.batch * capacity), tiles = (rows + 63) / 64;
         auto split = [&](int keys) {
             p.keys = keys;
@@ -255,8 +256,6 @@ int ftcnn_low_rank_add(const ftcnn_low_rank_desc *d, const void *y, const void *
     g.rank = d->rank;
     g.groups = pl.groups;
     g.splits = pl.splits;
-    g.tiles = pl.tiles;
-    g.together = pl.together;
     g.div_splits = fast_div((uint32_t)pl.splits);
     g.ways = pl.ways;
     g.expand_ways = pl.expand_ways;
@@ -317,7 +316,6 @@ int ftcnn_attention_mass(const ftcnn_mass_desc *d, const void *q, const void *k_
     t.capacity = (int)capacity;
     t.causal = d->causal != 0;
     t.window = (int)std::min<long long>(d->window, capacity);   // a wider one hides nothing more
-    t.tile_keys = 1;
     t.div_page = fast_div((uint32_t)d->page);
     t.div_group = fast_div((uint32_t)t.group);
     t.scale_log2 = d->scale * kLog2E;
