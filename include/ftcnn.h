@@ -541,9 +541,10 @@ typedef struct {
  * projection that all tokens share, A [adapters][rank][ch], B [adapters][m][rank].  ids [tokens] may come in
  * any order; a token whose id is not in [0, adapters) (none: -1) keeps y as it is.  scales (fp32
  * [adapters], NULL: 1).  ranks [adapters] (NULL: rank): adapter a has the first ranks[a] rows of A_a and
- * columns of B_a, taken within [0, rank]; what lies past them is not used.  A_a x_t is held in fp32; bf16:
- * for the second product as the sum of two bf16 values, within 2^-16 of it.  Infinities and NaN of a token
- * or adapter reach only the tokens that have them.  An infinity in B comes out as itself or as NaN.
+ * columns of B_a, taken within [0, rank]; what lies past them is not used, and may be anything where a rank is
+ * padded to 16 bytes.  A_a x_t is held in fp32; bf16: for the second product as the sum of two bf16 values, within
+ * 2^-17 of it (below 2^-117: within 2^-134).  Infinities and NaN of a token or adapter reach only the tokens that
+ * have them.  An infinity in B comes out as itself or as NaN.
  * out may be y (with its strides); outputs that overlap inputs otherwise are undefined.  Rows start on 16
  * bytes.  The workspace holds the products A x and, of many tokens, which have the same adapter.  The result does
  * not depend on timing.  One launch for few tokens, two, or three where many are grouped. */

@@ -31,9 +31,9 @@ def low_rank_add(y: torch.Tensor, x: torch.Tensor, a: torch.Tensor, b: torch.Ten
                  stream=None) -> torch.Tensor:
     """ftcnn_low_rank_add: y[t] + scales[i] * b[i] @ (a[i] @ x[t]) with i = ids[t] (int32 [tokens]; -1: no adapter).
     y [tokens][m], x [tokens][ch], a [adapters][rank][ch] and b [adapters][m][rank] are all float32 or bfloat16, strided as
-    they come with the last dimension contiguous; scales float32 [adapters]; ranks int32 [adapters], where
-    adapters use fewer than rank.  The output is allocated, contiguous, unless given (in place: out=y).  workspace:
-    uint8, 256-byte aligned; allocated when not given."""
+    they come with the last dimension contiguous; scales float32 [adapters]; ranks int32 [adapters], where adapters use
+    fewer than rank, which is a multiple of 4 (float32) or 8 (bfloat16), at most 128.  The output is allocated, contiguous,
+    unless given (in place: out=y).  workspace: uint8, 256-byte aligned; allocated when not given."""
     what = "low_rank_add"
     dtype, shape, dev = y.dtype, y.shape, y.get_device()
     if dtype not in _DTYPE or len(shape) != 2 or dev < 0:

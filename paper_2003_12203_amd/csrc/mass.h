@@ -17,7 +17,7 @@ struct MassArgs {
 };
 struct MassPlan {
     int dp;                      // head size the kernel is compiled for
-    bool wide;                   // more than 16 rows of a key head
+    bool wide;                   // more than 64 rows of a key head
     int keys;                    // of a workgroup
     int blocks, head_parts, row_parts;
     size_t bytes;

@@ -10,16 +10,17 @@
 // where there would be too few workgroups), tiles of 64 rows (fewer where heads are large) go through LDS, which the
 // workgroup's waves share, and the scores of the next 32 rows go through the matrix cores while these rows' weights are
 // made.  What bounds it with many rows is the vector unit beside the matrix cores: for each weight an argument, a power and a
-// sum, 16 cycles of it for every 24 that the matrix cores take for heads of 128, and the two overlap in part.  Two prompts of 8192 tokens, 32 heads of 128 over eight key heads,
-// bf16: 548 us, 1000 TFLOP/s of the 1260 that a product of 8192 x 8192 matrices reaches; as first written, with the weights after the
+// sum, 16 cycles of it for every 16 that the matrix cores take for heads of 128, and the two overlap in part (by counters the matrix cores
+// are busy for 51 % of the time, the vector unit, which issues for both, for 68 %).  Two prompts of 8192 tokens, 32 heads of 128 over eight key
+// heads, bf16: 548 us, 1000 TFLOP/s of the 1260 that a product of 8192 x 8192 matrices reaches; as first written, with the weights after the
 // scores, places divided for each row and lanes added through LDS, which spilled registers, 760.
 // 49 tokens over 70440 keys, 64 heads of 96 over eight: 94 us (125 with a mask in every tile that is not full).
 // Short calls pay for a workgroup's start, 8 us from its lengths to its sums.
 //
 // mass_few_kernel: the reading of the keys is all, straight into registers in the order of the matrix instructions; a
 // wave takes every fourth head of a run of keys, the next head's keys on their way.  64 single tokens, ragged, over up
-// to 8192 keys, 32 heads of 128 over eight, bf16, 102 MB: 25 us, 4.1 TB/s (a workgroup for every 64 keys that a sequence might have: 46);
-// one token over 131072, 268 MB: 54 us, 5.0 TB/s of the 5.2 of a large copy.  16 tokens of each of four sequences of 30016 keys (64 rows of a
+// to 8192 keys, 32 heads of 128 over eight, bf16, 102 MB: 25 us, 4.1 TB/s (a workgroup for every 64 keys that a sequence might have: 46; fp32,
+// 204 MB: 50); one token over 131072, 268 MB: 54 us, 5.0 TB/s of the 5.2 of a large copy (fp32 108).  16 tokens of each of four sequences of 30016 keys (64 rows of a
 // key head) 82 us, in the wide kernel 118.
 #pragma once
 
@@ -167,8 +168,6 @@ template <typename T, int DP, int KS> struct MassKeys {
     }
 };
 
-// The rows of a sequence that may see some keys, in tiles of ROWS.  Where the sequence has so many new tokens, a tile has
-// tokens of one query head (places in scalars); fewer are taken with their query heads one after the other.
 // How a tile's rows lie: those of one query head (by_head), or of all of the key head's, tokens' heads together, as 1 << shift of
 // them divide a tile's rows (other groups, of few tokens: shift -1).  By heads (two prompts of 8192 tokens 581 us; tokens' heads
 // together 595) unless the last tile of each, which is not full, would be another 15th.
@@ -182,6 +181,7 @@ template <int ROWS> struct MassOrder {
         if (by_head) shift = 0;
     }
 };
+// The rows of a sequence that may see keys of [k0, k1), in tiles of ROWS.
 template <int ROWS> struct MassTiles {
     bool by_head;
     int first, last;   // tiles of a query head, or of rows
